@@ -58,7 +58,13 @@ enum wash_status {
 };
 enum wash_layout { WASH_LAYOUT_NP = 0 /* [N][padded_P] */, WASH_LAYOUT_PN = 1 /* [padded_P][N] */ };
 enum wash_dtype { WASH_F32 = 0, WASH_BF16 = 1 };
-enum wash_stack { WASH_STACK_PARAMS = 0, WASH_STACK_OPT = 1 };
+enum wash_stack {
+    WASH_STACK_PARAMS = 0,
+    WASH_STACK_OPT = 1,   /* optimizer state: SGD's momentum, Adam's first moment                 */
+    /* 2 is WASH_STACK_BOTH, below */
+    WASH_STACK_GRADS = 3, /* the models' gradients                                                */
+    WASH_STACK_OPT2 = 4   /* Adam's second moment                                                 */
+};
 enum wash_schedule { WASH_SCHEDULE_DECREASING = 0, WASH_SCHEDULE_CONSTANT = 1, WASH_SCHEDULE_INCREASING = 2 };
 enum wash_mode {
     WASH_MODE_STREAM = 0, /* one pass that reads the whole stack and writes the selected
@@ -121,8 +127,8 @@ int wash_destroy(wash_ctx *ctx);
 int wash_stack_elems(const wash_ctx *ctx, int64_t *padded_P, int64_t *offsets);
 
 /* Lend a DEVICE buffer of n_elems == N * padded_P elements of `dtype` to the context
- * as its parameter stack or optimizer-state stack.  The pointer must be 16-byte
- * aligned.  Passing dev_ptr == NULL unbinds. */
+ * as its parameter stack, optimizer-state stack, gradient stack or second-moment stack.  The
+ * pointer must be 16-byte aligned.  Passing dev_ptr == NULL unbinds. */
 int wash_bind(wash_ctx *ctx, int32_t stack, int32_t dtype, void *dev_ptr, int64_t n_elems);
 
 /* Which kernel family the shuffle entry points launch (default WASH_MODE_STREAM).
@@ -234,6 +240,65 @@ int papa_all(wash_ctx *ctx, int32_t stack, void *stream);
  * binary64.  dev_sq_out is a DEVICE array of N doubles the caller has zeroed. */
 int wash_consensus_sq(wash_ctx *ctx, int32_t stack, int32_t tensor_lo, int32_t tensor_hi,
                       double *dev_sq_out, void *stream);
+
+/* ---- the optimizer's side of a training step --------------------------------------- *
+ *
+ * What a training loop does between the backward pass and the shuffle, for the N models at once: the gradients
+ * of all models lie in a stack of their own (WASH_STACK_GRADS, fp32 or bf16, same geometry and layout as the weights),
+ *
+ *   wash_grad_norm  ->  wash_sgd_step or wash_adamw_step  ->  wash_shuffle*
+ *
+ * Every model has its own gradient norm and its own clipping factor.  All calls are kernel launches on `stream` and can be captured into a
+ * graph; a graph holds the arguments of its calls (learning rate, step), but reads dev_norm, the stacks and the table of wash_set_decay as they
+ * are when it is replayed.  wash_grad_norm uses a workspace of the context: calls of one context, replayed graphs that hold them among those, must
+ * not overlap on the GPU.  wash_set_mode and wash_set_launch do not apply. */
+
+/* The gradient norm of every model over tensors [tensor_lo, tensor_hi):
+ *     dev_norm_out[n] = sqrt( sum_i g_n,i^2 )
+ * squares, sums and root in binary64.  dev_norm_out is a DEVICE array of N doubles, overwritten; an empty range gives 0.  The
+ * order of the additions depends on shape and device only, so equal gradients give equal bits.  A NaN among the gradients
+ * makes its model's norm NaN, an infinity (without a NaN) makes it infinite.  Shards of a population (wash_create_segments): square the shards' norms, add them, take the root. */
+int wash_grad_norm(wash_ctx *ctx, int32_t tensor_lo, int32_t tensor_hi, double *dev_norm_out, void *stream);
+
+/* Clips the gradients in place, each model by its own norm:
+ *     c_n = min(1, max_norm / (dev_norm[n] + 1e-6)), rounded to binary32;   g_n <- c_n g_n
+ * dev_norm: DEVICE array of N doubles (from wash_grad_norm); max_norm: finite, not negative.  Models with c_n = 1 are not touched.  A
+ * norm that is NaN makes its model's gradients NaN, an infinite one makes them 0 (NaN where they are infinite).  bf16 gradients are
+ * widened, multiplied and rounded to nearest even.  A step below takes the factor itself; this call is for other consumers of the gradients. */
+int wash_clip_grads(wash_ctx *ctx, double max_norm, const double *dev_norm, void *stream);
+
+/* Multipliers of the steps' weight decay, one per tensor (HOST array of n_tensors, finite, not negative; NULL: 1 for all, as in a new
+ * context): 0 leaves a tensor (a bias, a norm's weight) undecayed.  State of the context, uploaded in stream order when it changes; WASH_ERR_STATE
+ * while `stream` is being captured. */
+int wash_set_decay(wash_ctx *ctx, const double *decay_layer, void *stream);
+
+enum wash_step_flags {
+    WASH_STEP_NESTEROV = 1,      /* wash_sgd_step only                                               */
+    WASH_STEP_SKIP_NONFINITE = 2 /* a model whose dev_norm is infinite or NaN keeps weights and state */
+};
+
+/* One step of SGD on every model, in place on the parameter stack and, with momentum, the optimizer-state stack:
+ *     d = c_n g + (weight_decay * decay_t) p;   m <- momentum m + d;   p <- p - lr u
+ * with u = m, with WASH_STEP_NESTEROV u = d + momentum m, and with momentum = 0 u = d (the optimizer-state stack is then
+ * neither needed nor touched).  Zeros are the state before the first step.
+ *   lr, weight_decay   not negative; momentum in [0,1)
+ *   dev_norm           DEVICE array of N doubles: c_n as in wash_clip_grads, with the gradients themselves left as they are;
+ *                      NULL: c_n = 1 and max_norm is ignored
+ * Evaluated in binary32, every operation rounded once and none fused, in the order written; weights and gradients are fp32 or bf16 (widened
+ * exactly; new weights rounded to nearest even, so that a change below half a unit in the last place of a bf16 weight is lost: lend an fp32 stack where that
+ * matters).  The state must be fp32 (WASH_ERR_UNSUPPORTED otherwise: a moving average in bf16 stops moving).  The stacks must not overlap (WASH_ERR_ARG). */
+int wash_sgd_step(wash_ctx *ctx, double lr, double momentum, double weight_decay, int32_t flags, double max_norm,
+                  const double *dev_norm, void *stream);
+
+/* One step of AdamW (decoupled weight decay) on every model, in place; first moments m in the optimizer-state stack, second moments v in
+ * WASH_STACK_OPT2.  step counts from 0, as in wash_shuffle; t = step + 1:
+ *     g' = c_n g;   m <- beta1 m + (1 - beta1) g';   v <- beta2 v + ((1 - beta2) g') g'
+ *     p <- p - lr ( (m / (1 - beta1^t)) / (sqrt(v) / sqrt(1 - beta2^t) + eps) + (weight_decay * decay_t) p )
+ * beta1, beta2 in [0,1), eps positive; the factors of the bias correction are computed in binary64 and multiplied in binary32.  Otherwise as wash_sgd_step.
+ * A shuffle exchanges the stacks that it is given: for WASH+Opt with Adam shuffle both moments (the second one through a context of its own
+ * that has it bound as a stack; equal seed, step and probabilities give it the same permutations). */
+int wash_adamw_step(wash_ctx *ctx, uint64_t step, double lr, double beta1, double beta2, double eps, double weight_decay,
+                    int32_t flags, double max_norm, const double *dev_norm, void *stream);
 
 /* ---- whole step over HOST buffers ------------------------------------------------- */
 

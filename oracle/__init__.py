@@ -77,6 +77,11 @@ def lib() -> ctypes.CDLL:
         L.wo_population_average.argtypes = [popp, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32]
         L.wo_papa_all.argtypes = [popp, ctypes.c_void_p, ctypes.c_int32]
         L.wo_consensus_sq.argtypes = [popp, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, f64p]
+        vp, i32, dbl, u64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_double, ctypes.c_uint64
+        L.wo_grad_norm.argtypes = [popp, vp, i32, i32, i32, f64p]
+        L.wo_clip_grads.argtypes = [popp, vp, i32, dbl, f64p]
+        L.wo_sgd_step.argtypes = [popp, vp, i32, vp, i32, vp, f64p, f64p, i32, i32, dbl, f64p]
+        L.wo_adamw_step.argtypes = [popp, u64, vp, i32, vp, i32, vp, vp, f64p, f64p, i32, dbl, f64p]
         L.wo_set_threads.argtypes = [ctypes.c_int]; L.wo_set_threads.restype = None
         i64p = ctypes.POINTER(ctypes.c_int64)
         L.wo_exchange_counts.argtypes = [popp, f64p, ctypes.c_uint64, ctypes.c_uint64, i64p, i64p]
@@ -226,6 +231,51 @@ def consensus_sq(pop: Population, stack: np.ndarray, seg_lo: int = 0, seg_hi: in
                              out.ctypes.data_as(ctypes.POINTER(ctypes.c_double))) != 0:
         raise ValueError("wo_consensus_sq: bad argument")
     return out
+
+
+def _f64(a):
+    if a is None:
+        return None, None
+    arr = np.ascontiguousarray(a, dtype=np.float64)
+    return arr, arr.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+
+
+def grad_norm(pop: Population, grads: np.ndarray, seg_lo: int = 0, seg_hi: int | None = None) -> np.ndarray:
+    _check_stack(pop, grads)
+    out = np.zeros(pop.N, dtype=np.float64)
+    if lib().wo_grad_norm(pop.ref(), grads.ctypes.data, _np_dtype_code(grads), seg_lo, pop.T if seg_hi is None else seg_hi, _f64(out)[1]) != 0:
+        raise ValueError("wo_grad_norm: bad argument")
+    return out
+
+
+def clip_grads(pop: Population, grads: np.ndarray, max_norm: float, norm) -> None:
+    _check_stack(pop, grads)
+    keep, p = _f64(norm)
+    if lib().wo_clip_grads(pop.ref(), grads.ctypes.data, _np_dtype_code(grads), max_norm, p) != 0:
+        raise ValueError("wo_clip_grads: bad argument")
+
+
+def sgd_step(pop: Population, params, grads, m, lr, momentum=0.0, weight_decay=0.0, decay=None, nesterov=False, skip=False, max_norm=0.0, norm=None):
+    for a in (params, grads) + ((m,) if m is not None else ()):
+        _check_stack(pop, a)
+    hyper, hp = _f64([lr, momentum, 0.0, 0.0, weight_decay])
+    dec, dp = _f64(np.ones(pop.T) if decay is None else decay)
+    keep, np_ = _f64(norm)
+    if lib().wo_sgd_step(pop.ref(), params.ctypes.data, _np_dtype_code(params), grads.ctypes.data, _np_dtype_code(grads),
+                         None if m is None else m.ctypes.data, hp, dp, int(nesterov), int(skip), max_norm, np_) != 0:
+        raise ValueError("wo_sgd_step: bad argument")
+
+
+def adamw_step(pop: Population, step, params, grads, m, v, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, decay=None, skip=False,
+               max_norm=0.0, norm=None):
+    for a in (params, grads, m, v):
+        _check_stack(pop, a)
+    hyper, hp = _f64([lr, beta1, beta2, eps, weight_decay])
+    dec, dp = _f64(np.ones(pop.T) if decay is None else decay)
+    keep, np_ = _f64(norm)
+    if lib().wo_adamw_step(pop.ref(), step, params.ctypes.data, _np_dtype_code(params), grads.ctypes.data, _np_dtype_code(grads), m.ctypes.data,
+                           v.ctypes.data, hp, dp, int(skip), max_norm, np_) != 0:
+        raise ValueError("wo_adamw_step: bad argument")
 
 
 def _p_seg(pop: Population, p_seg) -> np.ndarray:

@@ -361,6 +361,111 @@ int wo_consensus_sq(const wo_population *pop, const void *stack, int32_t dtype,
     return WO_OK;
 }
 
+/* ---- the optimizer's side of a training step, every model by itself ----
+ * Not in the paper, whose experiments train with SGD and momentum ("Experimental setup"): textbook statements.
+ *   wo_grad_norm   norm_n = sqrt(sum_i g_n,i^2) over segments seg_lo .. seg_hi-1, in binary64
+ *   wo_clip_grads  g_n <- c_n g_n,  c_n = min(1, max_norm / (norm_n + 1e-6)) rounded to binary32; rows with c_n = 1 untouched
+ *   wo_sgd_step    d = c g + wd p;  m <- mu m + d;  p <- p - lr u,  u = m | d + mu m (nesterov) | d (mu = 0)
+ *   wo_adamw_step  Loshchilov and Hutter, "Decoupled weight decay regularization", Algorithm 2, with the bias
+ *                  correction of Kingma and Ba, "Adam"; t = step + 1
+ * binary32, one rounding an operation, in the order written.  decay[s] multiplies the weight decay of segment s.  norm == NULL: nothing
+ * is clipped; skip: models whose norm is not finite keep everything. */
+int wo_grad_norm(const wo_population *pop, const void *grads, int32_t dtype, int32_t seg_lo, int32_t seg_hi, double *norm)
+{
+    if (wo_check_pop(pop) != WO_OK || !grads || !norm) return WO_ERR_ARG;
+    if (seg_lo < 0 || seg_hi > pop->T || seg_lo > seg_hi) return WO_ERR_ARG;
+    for (int n = 0; n < pop->N; ++n) {
+        double sum = 0.0;
+        for (int s = seg_lo; s < seg_hi; ++s)
+            for (int64_t c = 0; c < pop->numel[s]; ++c) {
+                double g = (double)wo_load(grads, dtype, wo_index(pop, n, pop->offset[s] + c));
+                sum += g * g;
+            }
+        norm[n] = sqrt(sum);
+    }
+    return WO_OK;
+}
+
+static float wo_clip_factor(double norm, double max_norm)
+{
+    double c = max_norm / (norm + 1e-6);
+    if (c > 1.0) c = 1.0;
+    return (float)c;
+}
+
+int wo_clip_grads(const wo_population *pop, void *grads, int32_t dtype, double max_norm, const double *norm)
+{
+    if (wo_check_pop(pop) != WO_OK || !grads || !norm) return WO_ERR_ARG;
+    for (int n = 0; n < pop->N; ++n) {
+        float factor = wo_clip_factor(norm[n], max_norm);
+        if (factor == 1.0f) continue;
+        for (int s = 0; s < pop->T; ++s)
+            for (int64_t c = 0; c < pop->numel[s]; ++c) {
+                size_t idx = wo_index(pop, n, pop->offset[s] + c);
+                wo_store(grads, dtype, idx, factor * wo_load(grads, dtype, idx));
+            }
+    }
+    return WO_OK;
+}
+
+/* adamw: hyper = {lr, beta1, beta2, eps, weight decay}; SGD: {lr, momentum, -, -, weight decay} */
+static int wo_step(const wo_population *pop, int adamw, int nesterov, uint64_t step, void *params, int32_t p_dtype, const void *grads,
+                   int32_t g_dtype, float *m, float *v, const double *hyper, const double *decay, int skip, double max_norm, const double *norm)
+{
+    if (wo_check_pop(pop) != WO_OK || !params || !grads || !hyper || !decay) return WO_ERR_ARG;
+    const float lr = (float)hyper[0], b1 = (float)hyper[1], b2 = (float)hyper[2], eps = (float)hyper[3];
+    const float keep1 = (float)(1.0 - hyper[1]), keep2 = (float)(1.0 - hyper[2]);
+    const long double t = (long double)step + 1.0L;
+    const float first = adamw ? (float)(1.0L / (1.0L - powl((long double)hyper[1], t))) : 0.0f;
+    const float second = adamw ? (float)(1.0L / sqrtl(1.0L - powl((long double)hyper[2], t))) : 0.0f;
+    for (int n = 0; n < pop->N; ++n) {
+        if (skip && norm && !isfinite(norm[n])) continue;
+        const float factor = norm ? wo_clip_factor(norm[n], max_norm) : 1.0f;
+        for (int s = 0; s < pop->T; ++s) {
+            const float wd = (float)hyper[4] * (float)decay[s];
+            for (int64_t c = 0; c < pop->numel[s]; ++c) {
+                const size_t idx = wo_index(pop, n, pop->offset[s] + c);
+                const float p = wo_load(params, p_dtype, idx);
+                const float g = factor * wo_load(grads, g_dtype, idx);
+                const float pull = wd * p;
+                float u;
+                if (adamw) {
+                    const float old1 = b1 * m[idx], new1 = keep1 * g;
+                    m[idx] = old1 + new1;
+                    const float old2 = b2 * v[idx], half = keep2 * g, new2 = half * g;
+                    v[idx] = old2 + new2;
+                    const float root = second * sqrtf(v[idx]), denom = root + eps, top = first * m[idx];
+                    const float ratio = top / denom;
+                    u = ratio + pull;
+                } else {
+                    u = g + pull;
+                    if (hyper[1] > 0.0) {
+                        const float old1 = b1 * m[idx];
+                        m[idx] = old1 + u;
+                        const float ahead = b1 * m[idx];
+                        u = nesterov ? u + ahead : m[idx];
+                    }
+                }
+                const float change = lr * u;
+                wo_store(params, p_dtype, idx, p - change);
+            }
+        }
+    }
+    return WO_OK;
+}
+
+int wo_sgd_step(const wo_population *pop, void *params, int32_t p_dtype, const void *grads, int32_t g_dtype, float *m, const double *hyper,
+                const double *decay, int32_t nesterov, int32_t skip, double max_norm, const double *norm)
+{
+    return wo_step(pop, 0, nesterov, 0, params, p_dtype, grads, g_dtype, m, NULL, hyper, decay, skip, max_norm, norm);
+}
+
+int wo_adamw_step(const wo_population *pop, uint64_t step, void *params, int32_t p_dtype, const void *grads, int32_t g_dtype, float *m, float *v,
+                  const double *hyper, const double *decay, int32_t skip, double max_norm, const double *norm)
+{
+    return wo_step(pop, 1, 0, step, params, p_dtype, grads, g_dtype, m, v, hyper, decay, skip, max_norm, norm);
+}
+
 /* ---- the shuffling step as the workers see it (one model per worker) ----
  * The paper's deployment keeps model n on worker n; a shuffled parameter travels
  * peer to peer along the permutation (Introduction: models communicate their

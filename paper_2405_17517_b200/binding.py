@@ -20,7 +20,8 @@ WASH_OK = 0
 WASH_ERR_ARG, WASH_ERR_STATE, WASH_ERR_ALLOC, WASH_ERR_CUDA, WASH_ERR_UNSUPPORTED, WASH_ERR_DEVICE_CHECK = -1, -2, -3, -4, -5, -6
 WASH_LAYOUT_NP, WASH_LAYOUT_PN = 0, 1
 WASH_F32, WASH_BF16 = 0, 1
-WASH_STACK_PARAMS, WASH_STACK_OPT, WASH_STACK_BOTH = 0, 1, 2
+WASH_STACK_PARAMS, WASH_STACK_OPT, WASH_STACK_BOTH, WASH_STACK_GRADS, WASH_STACK_OPT2 = 0, 1, 2, 3, 4
+WASH_STEP_NESTEROV, WASH_STEP_SKIP_NONFINITE = 1, 2
 WASH_MAX_CONSENSUS_RANGES = 8
 WASH_SCHEDULE_DECREASING, WASH_SCHEDULE_CONSTANT, WASH_SCHEDULE_INCREASING = 0, 1, 2
 WASH_MODE_STREAM, WASH_MODE_SPARSE, WASH_MODE_AUTO = 0, 1, 2
@@ -69,6 +70,11 @@ def load() -> ctypes.CDLL:
     L.population_average.argtypes = [vp, i32, vp, i32, vp]
     L.papa_all.argtypes = [vp, i32, vp]
     L.wash_consensus_sq.argtypes = [vp, i32, i32, i32, vp, vp]
+    L.wash_grad_norm.argtypes = [vp, i32, i32, vp, vp]
+    L.wash_clip_grads.argtypes = [vp, dbl, vp, vp]
+    L.wash_set_decay.argtypes = [vp, dblp, vp]
+    L.wash_sgd_step.argtypes = [vp, dbl, dbl, dbl, i32, dbl, vp, vp]
+    L.wash_adamw_step.argtypes = [vp, u64, dbl, dbl, dbl, dbl, dbl, i32, dbl, vp, vp]
     L.wash_step_host.argtypes = [vp, i32, vp, vp, vp, u64, dbl, dblp, u64, ctypes.c_float, vp, ctypes.POINTER(wash_stats)]
     L.wash_check.argtypes = [vp, vp]
     L.wash_philox_probe.argtypes = [u64, u64, vp, i32, vp]
@@ -231,6 +237,32 @@ def papa_all(ctx, stack: int, stream=None) -> None:
 
 def wash_consensus_sq(ctx, stack: int, tensor_lo: int, tensor_hi: int, dev_sq_out, stream=None) -> None:
     _check(load().wash_consensus_sq(ctx, stack, tensor_lo, tensor_hi, _ptr(dev_sq_out), _stream(stream)))
+
+
+def wash_grad_norm(ctx, tensor_lo: int, tensor_hi: int, dev_norm_out, stream=None) -> None:
+    """dev_norm_out: [N] doubles on the device, overwritten"""
+    _check(load().wash_grad_norm(ctx, tensor_lo, tensor_hi, _ptr(dev_norm_out), _stream(stream)))
+
+
+def wash_clip_grads(ctx, max_norm: float, dev_norm, stream=None) -> None:
+    _check(load().wash_clip_grads(ctx, float(max_norm), _ptr(dev_norm), _stream(stream)))
+
+
+def wash_set_decay(ctx, decay_layer=None, stream=None) -> None:
+    """decay_layer: a multiplier of the steps' weight decay per tensor; None: 1 for all"""
+    keep, dl = _dbl_or_null(decay_layer)
+    _check(load().wash_set_decay(ctx, dl, _stream(stream)))
+
+
+def wash_sgd_step(ctx, lr: float, momentum: float = 0.0, weight_decay: float = 0.0, flags: int = 0, max_norm: float = 0.0,
+                  dev_norm=None, stream=None) -> None:
+    _check(load().wash_sgd_step(ctx, float(lr), float(momentum), float(weight_decay), flags, float(max_norm), _ptr(dev_norm), _stream(stream)))
+
+
+def wash_adamw_step(ctx, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+                    flags: int = 0, max_norm: float = 0.0, dev_norm=None, stream=None) -> None:
+    _check(load().wash_adamw_step(ctx, step, float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), flags, float(max_norm),
+                                  _ptr(dev_norm), _stream(stream)))
 
 
 def wash_step_host(ctx, ops: int, host_params, host_opt, host_avg, step, p, p_layer=None, seed=0, alpha=0.5,

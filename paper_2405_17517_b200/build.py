@@ -18,8 +18,8 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libwash.so")
 
-UNITS = ("wash_shuffle", "wash_shuffle_loop", "wash_shuffle_wide", "wash_shuffle_sparse", "wash_reduce_f32", "wash_reduce_bf16", "wash_exchange",
-         "wash_dispatch", "wash_noalloc", "wash_api")   # slowest first
+UNITS = ("wash_shuffle", "wash_shuffle_loop", "wash_shuffle_wide", "wash_shuffle_sparse", "wash_reduce_f32", "wash_reduce_bf16", "wash_step", "wash_exchange",
+         "wash_dispatch", "wash_noalloc", "wash_grad_norm", "wash_clip", "wash_api")   # slowest first
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]

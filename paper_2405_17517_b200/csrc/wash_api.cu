@@ -40,6 +40,7 @@ int cuda_fail(cudaError_t err, const char *what)
     return fail(WASH_ERR_CUDA, "%s: %s", what, cudaGetErrorString(err));
 }
 
+constexpr int kStacks = WASH_STACK_OPT2 + 1;
 constexpr int kSlots = 4;   // pinned staging slots for table uploads
 // Expected share of selected coordinates from which the streaming kernel's early flavour is launched (N > 16) instead of the
 // wide kernel.  2^24 coordinates, fp32, N = 32, wide / early at 50 / 70 / 100 %: [N][P] 559 / 647, 693 / 690, 895 / 665 us; [P][N] 659 / 960, 838 / 867,
@@ -91,8 +92,10 @@ struct wash_ctx {
     bool slot_used[kSlots] = {false, false, false, false};
     int next_slot = 0;
 
-    void *stack_ptr[2] = {nullptr, nullptr};
-    int stack_dtype[2] = {0, 0};
+    void *stack_ptr[kStacks] = {};         // by enum wash_stack; entry WASH_STACK_BOTH stays unused
+    int stack_dtype[kStacks] = {};
+    double *norm_partial_dev = nullptr;    // wash_grad_norm: the blocks' partial sums; behind them
+    uint32_t *norm_ticket_dev = nullptr;   // the number of blocks that have reported, 0 between calls
 
     uint32_t *status_dev = nullptr;
     wash_stats *stats_dev = nullptr;       // for wash_step_host
@@ -134,6 +137,7 @@ void release(wash_ctx *ctx)
     if (ctx->status_dev) cudaFree(ctx->status_dev);
     if (ctx->stats_dev) cudaFree(ctx->stats_dev);
     if (ctx->stat_slots_dev) cudaFree(ctx->stat_slots_dev);
+    if (ctx->norm_partial_dev) cudaFree(ctx->norm_partial_dev);
     if (ctx->avg_dev) cudaFree(ctx->avg_dev);
     if (ctx->x_mask) cudaFree(ctx->x_mask);
     if (ctx->x_block_total) cudaFree(ctx->x_block_total);
@@ -231,6 +235,26 @@ double sparse_share(int layout, int N, bool two_stacks, bool bf16)
     return N <= 12 ? 0.18 : N <= 16 ? 0.5 : N <= 24 ? 0.3 : 0.36;
 }
 
+// Copies the host mirror of the segment table to the device, in stream order.
+int upload_table(wash_ctx *ctx, cudaStream_t stream)
+{
+    const int slot = ctx->next_slot;
+    ctx->next_slot = (slot + 1) % kSlots;
+    if (ctx->slot_used[slot]) {   // the copy that last read this slot must be done
+        cudaError_t err = cudaEventSynchronize(ctx->slot_event[slot]);
+        if (err != cudaSuccess) return cuda_fail(err, "cudaEventSynchronize(table slot)");
+    }
+    const size_t bytes = sizeof(SegEntry) * static_cast<size_t>(ctx->n_seg);
+    std::memcpy(ctx->seg_pinned[slot], ctx->seg_host.data(), bytes);
+    cudaError_t err = cudaMemcpyAsync(ctx->seg_dev, ctx->seg_pinned[slot], bytes, cudaMemcpyHostToDevice, stream);
+    if (err != cudaSuccess) return cuda_fail(err, "cudaMemcpyAsync(segment table)");
+    err = cudaEventRecord(ctx->slot_event[slot], stream);
+    if (err != cudaSuccess) return cuda_fail(err, "cudaEventRecord(table slot)");
+    ctx->slot_used[slot] = true;
+    ctx->seg_uploaded = true;
+    return WASH_OK;
+}
+
 // Brings the device copy of the segment table up to date with the call's
 // probabilities (uploaded, in stream order, only when they changed).
 int sync_table(wash_ctx *ctx, double p, const double *p_layer, cudaStream_t stream)
@@ -254,21 +278,7 @@ int sync_table(wash_ctx *ctx, double p, const double *p_layer, cudaStream_t stre
     ctx->expected_selected = 0.0;
     for (int s = 0; s < ctx->n_seg; ++s)
         ctx->expected_selected += static_cast<double>(ctx->seg_host[s].numel) * static_cast<double>(ctx->seg_host[s].thr) / 4294967296.0;
-    const int slot = ctx->next_slot;
-    ctx->next_slot = (slot + 1) % kSlots;
-    if (ctx->slot_used[slot]) {   // the copy that last read this slot must be done
-        cudaError_t err = cudaEventSynchronize(ctx->slot_event[slot]);
-        if (err != cudaSuccess) return cuda_fail(err, "cudaEventSynchronize(table slot)");
-    }
-    const size_t bytes = sizeof(SegEntry) * static_cast<size_t>(ctx->n_seg);
-    std::memcpy(ctx->seg_pinned[slot], ctx->seg_host.data(), bytes);
-    cudaError_t err = cudaMemcpyAsync(ctx->seg_dev, ctx->seg_pinned[slot], bytes, cudaMemcpyHostToDevice, stream);
-    if (err != cudaSuccess) return cuda_fail(err, "cudaMemcpyAsync(segment table)");
-    err = cudaEventRecord(ctx->slot_event[slot], stream);
-    if (err != cudaSuccess) return cuda_fail(err, "cudaEventRecord(table slot)");
-    ctx->slot_used[slot] = true;
-    ctx->seg_uploaded = true;
-    return WASH_OK;
+    return upload_table(ctx, stream);
 }
 
 // [P][N]: a vector of padding after a group of the streaming kernels' shared-memory image, against bank conflicts.  It
@@ -417,6 +427,76 @@ int reduce_impl(wash_ctx *ctx, int op, int stack, void *out, int out_dtype, floa
     return WASH_OK;
 }
 
+// a non-negative number that binary32 holds (rounded)
+bool fits_f32(double x) { return x >= 0.0 && x <= 3.4028234663852886e38; }
+
+bool capturing(cudaStream_t stream)
+{
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    const cudaError_t err = cudaStreamIsCapturing(stream, &status);
+    if (err != cudaSuccess) cudaGetLastError();   // the default stream, while another one is being captured
+    return err != cudaSuccess || status != cudaStreamCaptureStatusNone;
+}
+
+// The segment table for a call of the optimizer's side.  It is on the device from wash_create on; only a failed upload leaves it to be copied again.
+int table_for_step(wash_ctx *ctx, cudaStream_t stream)
+{
+    if (ctx->seg_uploaded) return WASH_OK;
+    if (capturing(stream)) return fail(WASH_ERR_STATE, "the context's table has to be uploaded, which a stream that is being captured cannot do");
+    return upload_table(ctx, stream);
+}
+
+int check_clipping(double max_norm, const double *dev_norm)
+{
+    if (!(max_norm >= 0.0 && max_norm <= 1.7976931348623157e308)) return fail(WASH_ERR_ARG, "max_norm is %g, not a finite non-negative number", max_norm);
+    if (reinterpret_cast<uintptr_t>(dev_norm) & 7) return fail(WASH_ERR_ARG, "dev_norm must be 8-byte aligned");
+    return WASH_OK;
+}
+
+// `args` holds the rule's own constants; the rest is filled in here.
+int step_impl(wash_ctx *ctx, wash::StepArgs &args, int rule, double lr, double weight_decay, int flags, double max_norm, const double *dev_norm, void *stream_v)
+{
+    if (!ctx) return fail(WASH_ERR_ARG, "ctx is NULL");
+    if (!fits_f32(lr)) return fail(WASH_ERR_ARG, "lr is %g, not a non-negative binary32 number", lr);
+    if (!fits_f32(weight_decay)) return fail(WASH_ERR_ARG, "weight_decay is %g, not a non-negative binary32 number", weight_decay);
+    int rc;
+    if (dev_norm && (rc = check_clipping(max_norm, dev_norm)) != WASH_OK) return rc;
+    if (!dev_norm && (flags & WASH_STEP_SKIP_NONFINITE)) return fail(WASH_ERR_ARG, "WASH_STEP_SKIP_NONFINITE needs dev_norm");
+    struct { int stack; const char *name; bool needed; } const used[] = {{WASH_STACK_PARAMS, "parameter", true}, {WASH_STACK_GRADS, "gradient", true},
+        {WASH_STACK_OPT, "optimizer-state", rule != wash::kRuleSgd}, {WASH_STACK_OPT2, "second-moment", rule == wash::kRuleAdamW}};
+    for (const auto &u : used) {
+        if (!u.needed) continue;
+        if (!ctx->stack_ptr[u.stack]) return fail(WASH_ERR_STATE, "%s stack is not bound", u.name);
+        if ((u.stack == WASH_STACK_OPT || u.stack == WASH_STACK_OPT2) && ctx->stack_dtype[u.stack] != WASH_F32)
+            return fail(WASH_ERR_UNSUPPORTED, "the %s stack of a step must be fp32", u.name);
+    }
+    const size_t n_elems = static_cast<size_t>(ctx->N) * static_cast<size_t>(ctx->padded_P);
+    for (const auto &u : used)
+        for (const auto &w : used) {
+            if (&u == &w || !u.needed || !w.needed) continue;
+            const uintptr_t at = reinterpret_cast<uintptr_t>(ctx->stack_ptr[u.stack]), other = reinterpret_cast<uintptr_t>(ctx->stack_ptr[w.stack]);
+            if (at <= other && other < at + n_elems * elem_bytes(ctx->stack_dtype[u.stack])) return fail(WASH_ERR_ARG, "%s and %s stack overlap", u.name, w.name);
+        }
+    DeviceGuard guard(ctx->device);
+    if (guard.err != cudaSuccess) return cuda_fail(guard.err, "cudaSetDevice");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    if ((rc = table_for_step(ctx, stream)) != WASH_OK) return rc;
+    args.pop = view_of(ctx);
+    args.params = ctx->stack_ptr[WASH_STACK_PARAMS];
+    args.grads = ctx->stack_ptr[WASH_STACK_GRADS];
+    args.m = rule != wash::kRuleSgd ? ctx->stack_ptr[WASH_STACK_OPT] : nullptr;
+    args.v = rule == wash::kRuleAdamW ? ctx->stack_ptr[WASH_STACK_OPT2] : nullptr;
+    args.norm = dev_norm;
+    args.max_norm = max_norm;
+    args.lr = static_cast<float>(lr);
+    args.decay = static_cast<float>(weight_decay);
+    args.skip_nonfinite = (flags & WASH_STEP_SKIP_NONFINITE) != 0;
+    args.status = ctx->status_dev;
+    cudaError_t err = wash::launch_step(args, rule, ctx->stack_dtype[WASH_STACK_PARAMS], ctx->stack_dtype[WASH_STACK_GRADS], stream);
+    if (err != cudaSuccess) return cuda_fail(err, "optimizer step launch");
+    return WASH_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -462,7 +542,7 @@ int wash_create_segments(wash_ctx **out, int32_t N, int32_t n_segments, const in
         e.tensor_id = ctx->tensor_id[s];
         e.cgroup_begin = static_cast<uint32_t>(ctx->coord_begin[s] / 4);
         e.numel = static_cast<uint32_t>(ctx->numel[s]);
-        e.reserved = 0;
+        e.decay = 1.f;
         e.thr = 0;
     }
     std::vector<uint32_t> tile_first(ctx->n_tiles);
@@ -484,11 +564,13 @@ int wash_create_segments(wash_ctx **out, int32_t N, int32_t n_segments, const in
     ctx->shape.sm_count = sm_count;
     const size_t seg_bytes = sizeof(SegEntry) * static_cast<size_t>(n_segments);
     const size_t slot_bytes = sizeof(wash::StatSlot) * (wash::kStatSlots + 1) + sizeof(double) * wash::kSqSlots * wash::kMaxSqRanges * static_cast<size_t>(N);
+    const size_t norm_bytes = sizeof(double) * wash::norm_partials(layout, N, sm_count);
     if ((err = cudaMalloc(&ctx->seg_dev, seg_bytes)) != cudaSuccess ||
         (err = cudaMalloc(&ctx->tile_first_dev, sizeof(uint32_t) * ctx->n_tiles)) != cudaSuccess ||
         (err = cudaMalloc(&ctx->status_dev, sizeof(uint32_t))) != cudaSuccess ||
         (err = cudaMalloc(&ctx->stats_dev, sizeof(wash_stats))) != cudaSuccess ||
-        (err = cudaMalloc(&ctx->stat_slots_dev, slot_bytes)) != cudaSuccess) {
+        (err = cudaMalloc(&ctx->stat_slots_dev, slot_bytes)) != cudaSuccess ||
+        (err = cudaMalloc(&ctx->norm_partial_dev, norm_bytes + sizeof(uint32_t))) != cudaSuccess) {
         release(ctx);
         cudaGetLastError();
         return fail(WASH_ERR_ALLOC, "device allocation failed: %s", cudaGetErrorString(err));
@@ -504,10 +586,19 @@ int wash_create_segments(wash_ctx **out, int32_t N, int32_t n_segments, const in
     if ((err = cudaMemcpy(ctx->tile_first_dev, tile_first.data(), sizeof(uint32_t) * ctx->n_tiles, cudaMemcpyHostToDevice)) != cudaSuccess ||
         (err = cudaMemset(ctx->status_dev, 0, sizeof(uint32_t))) != cudaSuccess ||
         (err = cudaMemset(ctx->stats_dev, 0, sizeof(wash_stats))) != cudaSuccess ||
-        (err = cudaMemset(ctx->stat_slots_dev, 0, slot_bytes)) != cudaSuccess) {
+        (err = cudaMemset(ctx->stat_slots_dev, 0, slot_bytes)) != cudaSuccess ||
+        (err = cudaMemset(ctx->norm_partial_dev, 0, norm_bytes + sizeof(uint32_t))) != cudaSuccess) {
         release(ctx);
         return cuda_fail(err, "table upload");
     }
+    // The segment table with nothing selected, from pinned memory: this copy has arrived when it returns, and what the default stream had before it, too.
+    std::memcpy(ctx->seg_pinned[0], ctx->seg_host.data(), seg_bytes);
+    if ((err = cudaMemcpy(ctx->seg_dev, ctx->seg_pinned[0], seg_bytes, cudaMemcpyHostToDevice)) != cudaSuccess) {
+        release(ctx);
+        return cuda_fail(err, "table upload");
+    }
+    ctx->seg_uploaded = true;
+    ctx->norm_ticket_dev = reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(ctx->norm_partial_dev) + norm_bytes);
     ctx->sq_slots_dev = reinterpret_cast<double *>(ctx->stat_slots_dev + wash::kStatSlots + 1);
     *out = ctx;
     return WASH_OK;
@@ -537,7 +628,7 @@ int wash_stack_elems(const wash_ctx *ctx, int64_t *padded_P, int64_t *offsets)
 int wash_bind(wash_ctx *ctx, int32_t stack, int32_t dtype, void *dev_ptr, int64_t n_elems)
 {
     if (!ctx) return fail(WASH_ERR_ARG, "ctx is NULL");
-    if (stack != WASH_STACK_PARAMS && stack != WASH_STACK_OPT) return fail(WASH_ERR_ARG, "stack must be 0 or 1");
+    if (stack < 0 || stack >= kStacks || stack == WASH_STACK_BOTH) return fail(WASH_ERR_ARG, "stack must be 0, 1, 3 or 4");
     if (!dev_ptr) { ctx->stack_ptr[stack] = nullptr; return WASH_OK; }
     if (dtype != WASH_F32 && dtype != WASH_BF16) return fail(WASH_ERR_ARG, "unknown dtype %d", dtype);
     if (n_elems != static_cast<int64_t>(ctx->N) * ctx->padded_P)
@@ -669,6 +760,108 @@ int wash_consensus_sq(wash_ctx *ctx, int32_t stack, int32_t tensor_lo, int32_t t
     if (err != cudaSuccess) return cuda_fail(err, "consensus kernel launch");
     if (!supported) return fail(WASH_ERR_UNSUPPORTED, "no kernel for dtype %d", ctx->stack_dtype[stack]);
     return WASH_OK;
+}
+
+int wash_grad_norm(wash_ctx *ctx, int32_t tensor_lo, int32_t tensor_hi, double *dev_norm_out, void *stream_v)
+{
+    if (!ctx) return fail(WASH_ERR_ARG, "ctx is NULL");
+    if (!dev_norm_out || (reinterpret_cast<uintptr_t>(dev_norm_out) & 7)) return fail(WASH_ERR_ARG, "dev_norm_out must be an 8-byte aligned device pointer");
+    if (tensor_lo < 0 || tensor_hi > ctx->n_seg || tensor_lo > tensor_hi) return fail(WASH_ERR_ARG, "tensor range [%d, %d) is not within [0, %d]", tensor_lo, tensor_hi, ctx->n_seg);
+    if (!ctx->stack_ptr[WASH_STACK_GRADS]) return fail(WASH_ERR_STATE, "gradient stack is not bound");
+    DeviceGuard guard(ctx->device);
+    if (guard.err != cudaSuccess) return cuda_fail(guard.err, "cudaSetDevice");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    int rc = table_for_step(ctx, stream);
+    if (rc != WASH_OK) return rc;
+    wash::NormArgs args = {};
+    args.pop = view_of(ctx);
+    args.grads = ctx->stack_ptr[WASH_STACK_GRADS];
+    if (tensor_lo < tensor_hi) {
+        args.unit_lo = ctx->seg_host[static_cast<size_t>(tensor_lo)].group_begin / 2;
+        args.unit_hi = ctx->seg_host[static_cast<size_t>(tensor_hi) - 1].group_end / 2;
+    }
+    args.partial = ctx->norm_partial_dev;
+    args.ticket = ctx->norm_ticket_dev;
+    args.out = dev_norm_out;
+    args.status = ctx->status_dev;
+    cudaError_t err = wash::launch_grad_norm(args, ctx->stack_dtype[WASH_STACK_GRADS], ctx->shape.sm_count, stream);
+    if (err != cudaSuccess) return cuda_fail(err, "gradient norm launch");
+    return WASH_OK;
+}
+
+int wash_clip_grads(wash_ctx *ctx, double max_norm, const double *dev_norm, void *stream_v)
+{
+    if (!ctx) return fail(WASH_ERR_ARG, "ctx is NULL");
+    if (!dev_norm) return fail(WASH_ERR_ARG, "dev_norm is NULL");
+    int rc = check_clipping(max_norm, dev_norm);
+    if (rc != WASH_OK) return rc;
+    if (!ctx->stack_ptr[WASH_STACK_GRADS]) return fail(WASH_ERR_STATE, "gradient stack is not bound");
+    DeviceGuard guard(ctx->device);
+    if (guard.err != cudaSuccess) return cuda_fail(guard.err, "cudaSetDevice");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    if ((rc = table_for_step(ctx, stream)) != WASH_OK) return rc;
+    wash::ClipArgs args = {};
+    args.pop = view_of(ctx);
+    args.grads = ctx->stack_ptr[WASH_STACK_GRADS];
+    args.norm = dev_norm;
+    args.max_norm = max_norm;
+    args.status = ctx->status_dev;
+    cudaError_t err = wash::launch_clip(args, ctx->stack_dtype[WASH_STACK_GRADS], ctx->shape.sm_count, stream);
+    if (err != cudaSuccess) return cuda_fail(err, "clipping launch");
+    return WASH_OK;
+}
+
+int wash_set_decay(wash_ctx *ctx, const double *decay_layer, void *stream_v)
+{
+    if (!ctx) return fail(WASH_ERR_ARG, "ctx is NULL");
+    if (decay_layer)
+        for (int s = 0; s < ctx->n_seg; ++s)
+            if (!fits_f32(decay_layer[s])) return fail(WASH_ERR_ARG, "decay multiplier of tensor %d is %g, not a non-negative binary32 number", s, decay_layer[s]);
+    DeviceGuard guard(ctx->device);
+    if (guard.err != cudaSuccess) return cuda_fail(guard.err, "cudaSetDevice");
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    if (capturing(stream)) return fail(WASH_ERR_STATE, "the decay multipliers cannot be set while the stream is being captured");
+    bool changed = !ctx->seg_uploaded;
+    for (int s = 0; s < ctx->n_seg; ++s) {
+        const float decay = decay_layer ? static_cast<float>(decay_layer[s]) : 1.f;
+        changed = changed || decay != ctx->seg_host[s].decay;
+        ctx->seg_host[s].decay = decay;
+    }
+    if (!changed) return WASH_OK;
+    ctx->seg_uploaded = false;   // until the copy is queued, the mirror is ahead of the device table
+    return upload_table(ctx, stream);
+}
+
+int wash_sgd_step(wash_ctx *ctx, double lr, double momentum, double weight_decay, int32_t flags, double max_norm, const double *dev_norm, void *stream)
+{
+    if (!(momentum >= 0.0 && momentum < 1.0)) return fail(WASH_ERR_ARG, "momentum is %g, not in [0,1)", momentum);
+    if (flags & ~(WASH_STEP_NESTEROV | WASH_STEP_SKIP_NONFINITE)) return fail(WASH_ERR_ARG, "unknown bits in flags");
+    if ((flags & WASH_STEP_NESTEROV) && momentum == 0.0) return fail(WASH_ERR_ARG, "Nesterov's form needs a momentum above 0");
+    wash::StepArgs args = {};
+    args.beta1 = static_cast<float>(momentum);
+    const int rule = flags & WASH_STEP_NESTEROV ? wash::kRuleNesterov : momentum > 0.0 ? wash::kRuleMomentum : wash::kRuleSgd;
+    return step_impl(ctx, args, rule, lr, weight_decay, flags, max_norm, dev_norm, stream);
+}
+
+int wash_adamw_step(wash_ctx *ctx, uint64_t step, double lr, double beta1, double beta2, double eps, double weight_decay, int32_t flags, double max_norm,
+                    const double *dev_norm, void *stream)
+{
+    if (step >> 56) return fail(WASH_ERR_ARG, "step must be below 2^56");
+    if (!(beta1 >= 0.0 && beta1 < 1.0)) return fail(WASH_ERR_ARG, "beta1 is %g, not in [0,1)", beta1);
+    if (!(beta2 >= 0.0 && beta2 < 1.0)) return fail(WASH_ERR_ARG, "beta2 is %g, not in [0,1)", beta2);
+    if (!(fits_f32(eps) && static_cast<float>(eps) > 0.f)) return fail(WASH_ERR_ARG, "eps is %g, not a positive binary32 number", eps);
+    if (flags & ~WASH_STEP_SKIP_NONFINITE) return fail(WASH_ERR_ARG, "unknown bits in flags");
+    wash::StepArgs args = {};
+    args.beta1 = static_cast<float>(beta1);
+    args.one_minus_beta1 = static_cast<float>(1.0 - beta1);
+    args.beta2 = static_cast<float>(beta2);
+    args.one_minus_beta2 = static_cast<float>(1.0 - beta2);
+    // 1 - beta^t, t = step + 1, without the difference of two neighbouring numbers
+    const double t = static_cast<double>(step) + 1.0;
+    args.first_scale = static_cast<float>(1.0 / -std::expm1(t * std::log(beta1)));
+    args.second_scale = static_cast<float>(1.0 / std::sqrt(-std::expm1(t * std::log(beta2))));
+    args.eps = static_cast<float>(eps);
+    return step_impl(ctx, args, wash::kRuleAdamW, lr, weight_decay, flags, max_norm, dev_norm, stream);
 }
 
 int wash_step_host(wash_ctx *ctx, int32_t ops, void *host_params, void *host_opt, void *host_avg, uint64_t step,

@@ -37,7 +37,7 @@ struct SegEntry {
     uint32_t tensor_id;     // RNG tensor index
     uint32_t cgroup_begin;  // (first coordinate's index within its tensor) / 4
     uint32_t numel;         // coordinates in the segment
-    uint32_t reserved;
+    float decay;            // the segment's multiplier of the optimizer's weight decay (wash_set_decay)
     uint64_t thr;           // floor(p * 2^32): coordinate selected iff word < thr
 };
 static_assert(sizeof(SegEntry) == 32, "SegEntry must stay 32 bytes");
@@ -223,6 +223,64 @@ struct ReduceArgs {
     uint32_t group_lo, group_hi;  // range of groups to process (both even: whole units of 8 elements)
     uint32_t *status;
 };
+
+// ---- the optimizer's side of a training step (wash_grad_norm, wash_clip_grads, wash_*_step) ----
+// A unit of work is an octet: 8 consecutive elements of a stack, which in [N][P] are 8 coordinates of one model (tensors start on multiples of 8 elements,
+// so they belong to one tensor) and in [P][N] the 8 N values of 8 coordinates cut into N octets.  A chunk is what kChunkThreads threads take
+// at a time, an octet each: 2048 coordinates of one model in [N][P], in [P][N] the octets of chunk_units(N) units of 8 coordinates, all models -- so that a
+// thread's octet holds the same models in every chunk.
+constexpr int kChunkThreads = 256;
+__host__ __device__ constexpr uint32_t chunk_units(int layout, int n_models)
+{
+    return layout == kLayoutNP ? kChunkThreads : static_cast<uint32_t>(kChunkThreads / n_models);
+}
+
+struct NormArgs {
+    PopView pop;
+    const void *grads;
+    uint32_t unit_lo, unit_hi;   // units of 8 coordinates to cover
+    uint32_t n_chunks;           // chunks they take
+    uint32_t per_model;          // blocks of a model ([N][P]); [P][N]: all blocks, every one of which has a part of every model
+    double *partial;             // [N][per_model]
+    uint32_t *ticket;            // blocks that have reported; 0 between launches
+    double *out;                 // [N]
+    uint32_t *status;
+};
+// Blocks of the norm's grid, and the partial sums they leave.
+constexpr int kNormBlocksNP = 8, kNormBlocksPN = 4;   // an SM
+inline size_t norm_partials(int layout, int n_models, int sm_count)
+{
+    const size_t n = static_cast<size_t>(n_models), sm = static_cast<size_t>(sm_count);
+    return layout == kLayoutNP ? kNormBlocksNP * sm + n : kNormBlocksPN * sm * n;
+}
+
+struct ClipArgs {
+    PopView pop;
+    void *grads;
+    const double *norm;
+    double max_norm;
+    uint32_t *status;
+};
+
+enum StepRule { kRuleSgd = 0, kRuleMomentum = 1, kRuleNesterov = 2, kRuleAdamW = 3 };
+struct StepArgs {
+    PopView pop;
+    void *params;
+    const void *grads;
+    void *m, *v;                 // fp32 stacks or nullptr
+    const double *norm;          // nullptr: nothing is clipped
+    double max_norm;
+    float lr, decay;
+    float beta1, one_minus_beta1;            // SGD: beta1 is the momentum
+    float beta2, one_minus_beta2;
+    float first_scale, second_scale, eps;    // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    int skip_nonfinite;          // models whose norm is not finite keep everything
+    uint32_t *status;
+};
+
+cudaError_t launch_grad_norm(NormArgs args, int dtype, int sm_count, cudaStream_t stream);
+cudaError_t launch_clip(const ClipArgs &args, int dtype, int sm_count, cudaStream_t stream);
+cudaError_t launch_step(const StepArgs &args, int rule, int params_dtype, int grads_dtype, cudaStream_t stream);
 
 // One model per device (wash_exchange_*): the row is one model of a population of pop.N.
 constexpr int kExchangeTileGroups = 128;   // a warp tile (wash_warp_tiles.cuh): 32 lanes x 4 groups = 512 coordinates

@@ -89,7 +89,7 @@ extern "C" int wash_shuffle_noalloc(int32_t N, int32_t n_tensors, const int64_t 
         e.tensor_id = static_cast<uint32_t>(t);
         e.cgroup_begin = 0;
         e.numel = static_cast<uint32_t>(d);
-        e.reserved = 0;
+        e.decay = 0.f;
         e.thr = static_cast<uint64_t>(std::floor(pt * 4294967296.0));
         coordinates += static_cast<double>(d);
         expected += static_cast<double>(d) * pt;

@@ -1,0 +1,136 @@
+// What the kernels on the optimizer's side of a training step share: octets of a stack's values, the place of an octet among the tensors,
+// and a model's clipping factor.
+#pragma once
+#include "wash_device.cuh"
+#include "wash_launch.cuh"
+
+namespace wash {
+
+// Eight consecutive elements, as raw words: two 16-byte vectors of fp32, one of bf16.
+template <class T>
+struct Octet {
+    static constexpr int kVecs = T::kBytes / 2;
+    uint4 v[kVecs];
+
+    __device__ __forceinline__ void load(const char *p)
+    {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i] = F32::load_group(p + 16 * i);
+    }
+    __device__ __forceinline__ void store(char *p) const
+    {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) *reinterpret_cast<uint4 *>(p + 16 * i) = v[i];
+    }
+    __device__ __forceinline__ uint32_t word(int i) const
+    {
+        const uint4 &x = v[i / 4];
+        return i % 4 == 0 ? x.x : i % 4 == 1 ? x.y : i % 4 == 2 ? x.z : x.w;
+    }
+    __device__ __forceinline__ float get(int q) const
+    {
+        if constexpr (T::kBytes == 4) return __uint_as_float(word(q));
+        else return __uint_as_float((q & 1) ? word(q / 2) & 0xFFFF0000u : word(q / 2) << 16);
+    }
+    __device__ __forceinline__ uint32_t raw(int q) const
+    {
+        if constexpr (T::kBytes == 4) return word(q);
+        else return (q & 1) ? word(q / 2) >> 16 : word(q / 2) & 0xFFFFu;
+    }
+    // the values of `r` whose bit is set in `active`, the others' bits as they are
+    __device__ __forceinline__ void put(const float (&r)[8], uint32_t active)
+    {
+        uint32_t w[4 * kVecs];
+#pragma unroll
+        for (int i = 0; i < 4 * kVecs; ++i) {
+            if constexpr (T::kBytes == 4) w[i] = (active >> i) & 1u ? __float_as_uint(r[i]) : word(i);
+            else {
+                const uint32_t fresh = BF16::pair_from_floats(r[2 * i], r[2 * i + 1]), two = (active >> (2 * i)) & 3u;
+                const uint32_t mask = (two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u);
+                w[i] = (fresh & mask) | (word(i) & ~mask);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+    __device__ __forceinline__ void store_some(char *p, uint32_t mask) const
+    {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            if ((mask >> q) & 1u) T::store_elem(p, q, raw(q));
+    }
+};
+
+// The tensor of coordinate e of a row (4 coordinates to a group of the tables).
+struct Place {
+    uint32_t seg;
+    long long begin, real_end, end;   // of the tensor's coordinates in the row; behind real_end comes padding
+    float decay;
+};
+__device__ __forceinline__ Place place_entry(const PopView &pop, uint32_t s)
+{
+    const uint4 lo = __ldg(reinterpret_cast<const uint4 *>(pop.seg + s));       // begin, end, tensor, cgroup_begin
+    const uint2 hi = __ldg(reinterpret_cast<const uint2 *>(pop.seg + s) + 2);   // numel, decay
+    Place at;
+    at.seg = s;
+    at.begin = 4ll * lo.x;
+    at.real_end = at.begin + hi.x;
+    at.end = 4ll * lo.y;
+    at.decay = __uint_as_float(hi.y);
+    return at;
+}
+__device__ __forceinline__ Place find_place(const PopView &pop, long long e, uint32_t *status)
+{
+    const uint32_t g = static_cast<uint32_t>(e >> 2);
+    uint32_t s = __ldg(pop.tile_first + (g >> kTileShift));
+    const uint32_t last = static_cast<uint32_t>(pop.n_seg) - 1u;
+    while (s < last && g >= __ldg(&pop.seg[s].group_end)) ++s;
+    Place at = place_entry(pop, s);
+    if (e < at.begin || e >= at.end) {   // table inconsistent with the row: report, touch nothing
+        if (status) atomicOr(status, 1u);
+        at.real_end = at.begin;
+    }
+    return at;
+}
+
+// [N][P]: which of the unit's 8 coordinates exist, and their tensor's decay.
+__device__ __forceinline__ uint32_t existing_np(const PopView &pop, long long e, uint32_t *status, float *decay)
+{
+    const Place at = find_place(pop, e, status);
+    *decay = at.decay;
+    const long long left = at.real_end - e;
+    return left >= 8 ? 0xFFu : left > 0 ? (1u << left) - 1u : 0u;
+}
+
+// [P][N]: the same for the octet whose first value is model `n`'s of coordinate e.  Its values may belong to more than one tensor.
+__device__ __forceinline__ uint32_t existing_pn(const PopView &pop, long long e, uint32_t n, uint32_t *status, float (&decay)[8])
+{
+    Place at = find_place(pop, e, status);
+    const uint32_t N = static_cast<uint32_t>(pop.N);
+    if (e + (n + 7u) / N < at.real_end) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) decay[q] = at.decay;
+        return 0xFFu;
+    }
+    uint32_t mask = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        if (e >= at.end && at.seg + 1u < static_cast<uint32_t>(pop.n_seg)) at = place_entry(pop, at.seg + 1u);
+        decay[q] = at.decay;
+        if (e >= at.begin && e < at.real_end) mask |= 1u << q;
+        if (++n == N) {
+            n = 0;
+            ++e;
+        }
+    }
+    return mask;
+}
+
+// A model's clipping factor: max_norm / (norm + 1e-6) in binary64, at most 1, rounded to binary32.  A norm that is NaN gives NaN, an infinite one 0.
+__device__ __forceinline__ float clip_factor(double norm, double max_norm)
+{
+    const double c = max_norm / (norm + 1e-6);
+    return c >= 1.0 ? 1.f : static_cast<float>(c);
+}
+
+}  // namespace wash

@@ -1,0 +1,158 @@
+// The optimizer's step for all models in one pass, with the clipping's factor folded into the read of the gradients:
+//   SGD    d = c g + wd_t p;  m <- mu m + d;  p <- p - lr u,  u = m, with Nesterov d + mu m, without momentum d
+//   AdamW  g' = c g;  m <- b1 m + (1 - b1) g';  v <- b2 v + (1 - b2) g'^2;
+//          p <- p - lr (s1 m / (s2 sqrt(v) + eps) + wd_t p),  s1 = 1 / (1 - b1^t), s2 = 1 / sqrt(1 - b2^t)
+// in binary32, every operation rounded once (explicit _rn intrinsics), bf16 weights rounded to nearest even at the store.
+#include "wash_octet.cuh"
+
+namespace wash {
+
+template <int RULE>
+__device__ __forceinline__ void update(const StepArgs &a, float c, float wd, float g, float &p, float &m, float &v)
+{
+    g = __fmul_rn(c, g);
+    const float pull = __fmul_rn(wd, p);
+    if constexpr (RULE == kRuleAdamW) {
+        m = __fadd_rn(__fmul_rn(a.beta1, m), __fmul_rn(a.one_minus_beta1, g));
+        v = __fadd_rn(__fmul_rn(a.beta2, v), __fmul_rn(__fmul_rn(a.one_minus_beta2, g), g));
+        const float denom = __fadd_rn(__fmul_rn(a.second_scale, __fsqrt_rn(v)), a.eps);
+        const float u = __fdiv_rn(__fmul_rn(a.first_scale, m), denom);
+        p = __fsub_rn(p, __fmul_rn(a.lr, __fadd_rn(u, pull)));
+    } else {
+        float u = __fadd_rn(g, pull);
+        if constexpr (RULE != kRuleSgd) {
+            m = __fadd_rn(__fmul_rn(a.beta1, m), u);
+            u = RULE == kRuleNesterov ? __fadd_rn(u, __fmul_rn(a.beta1, m)) : m;
+        }
+        p = __fsub_rn(p, __fmul_rn(a.lr, u));
+    }
+}
+
+// A model's factor for a step: -1 (no factor is negative) where the model is to keep everything.
+__device__ __forceinline__ float step_factor(const StepArgs &a, uint32_t n)
+{
+    if (!a.norm) return 1.f;
+    const double norm = a.norm[n];
+    if (a.skip_nonfinite && !(norm <= 1.7976931348623157e308)) return -1.f;
+    return clip_factor(norm, a.max_norm);
+}
+
+template <class TW, class TG, int RULE>
+struct StepOctet {
+    Octet<TW> p;
+    Octet<TG> g;
+    Octet<F32> m, v;
+    __device__ __forceinline__ void load(const StepArgs &a, size_t element)
+    {
+        p.load(static_cast<const char *>(a.params) + element * TW::kBytes);
+        g.load(static_cast<const char *>(a.grads) + element * TG::kBytes);
+        if constexpr (RULE != kRuleSgd) m.load(static_cast<const char *>(a.m) + element * 4);
+        if constexpr (RULE == kRuleAdamW) v.load(static_cast<const char *>(a.v) + element * 4);
+    }
+    // mask: values that exist; active: values whose model is updated
+    __device__ __forceinline__ void finish(const StepArgs &a, size_t element, const float (&c)[8], const float (&wd)[8], uint32_t mask, uint32_t active)
+    {
+        float rp[8], rm[8], rv[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            rp[q] = p.get(q);
+            rm[q] = RULE != kRuleSgd ? m.get(q) : 0.f;
+            rv[q] = RULE == kRuleAdamW ? v.get(q) : 0.f;
+            update<RULE>(a, c[q], wd[q], g.get(q), rp[q], rm[q], rv[q]);
+        }
+        p.put(rp, active);
+        if constexpr (RULE != kRuleSgd) m.put(rm, active);
+        if constexpr (RULE == kRuleAdamW) v.put(rv, active);
+        char *pp = static_cast<char *>(a.params) + element * TW::kBytes, *pm = static_cast<char *>(a.m) + element * 4, *pv = static_cast<char *>(a.v) + element * 4;
+        if (mask == 0xFFu) {
+            p.store(pp);
+            if constexpr (RULE != kRuleSgd) m.store(pm);
+            if constexpr (RULE == kRuleAdamW) v.store(pv);
+        } else {
+            mask &= active;
+            p.store_some(pp, mask);
+            if constexpr (RULE != kRuleSgd) m.store_some(pm, mask);
+            if constexpr (RULE == kRuleAdamW) v.store_some(pv, mask);
+        }
+    }
+};
+
+template <class TW, class TG, int RULE>
+__global__ void __launch_bounds__(kChunkThreads) step_np_kernel(const __grid_constant__ StepArgs a)
+{
+    await_previous();
+    let_next_start();
+    const uint32_t N = static_cast<uint32_t>(a.pop.N), chunk = blockIdx.x / N, n = blockIdx.x - chunk * N;
+    const uint32_t unit = chunk * kChunkThreads + threadIdx.x;
+    if (unit >= a.pop.n_groups / 2) return;
+    const size_t element = static_cast<size_t>(n) * a.pop.padded_P + 8ull * unit;
+    StepOctet<TW, TG, RULE> o;
+    o.load(a, element);
+    const float factor = step_factor(a, n);
+    if (factor < 0.f) return;
+    float c[8], wd[8], decay;
+    const uint32_t mask = existing_np(a.pop, 8ll * unit, a.status, &decay);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        c[q] = factor;
+        wd[q] = __fmul_rn(a.decay, decay);
+    }
+    o.finish(a, element, c, wd, mask, 0xFFu);
+}
+
+template <class TW, class TG, int RULE>
+__global__ void __launch_bounds__(kChunkThreads) step_pn_kernel(const __grid_constant__ StepArgs a)
+{
+    await_previous();
+    let_next_start();
+    const uint32_t N = static_cast<uint32_t>(a.pop.N), units = chunk_units(kLayoutPN, a.pop.N);
+    const uint32_t first = blockIdx.x * units, here = min(units, a.pop.n_groups / 2 - first) * N;
+    const size_t element = (static_cast<size_t>(first) * N + threadIdx.x) * 8;
+    StepOctet<TW, TG, RULE> o;
+    if (threadIdx.x < here) o.load(a, element);
+    __shared__ float factor[kMaxN];
+    if (threadIdx.x < N) factor[threadIdx.x] = step_factor(a, threadIdx.x);
+    __syncthreads();
+    if (threadIdx.x >= here) return;
+    const uint32_t e0 = 8u * threadIdx.x / N, n0 = 8u * threadIdx.x - e0 * N;
+    float c[8], wd[8];
+    const uint32_t mask = existing_pn(a.pop, 8ll * first + e0, n0, a.status, wd);
+    uint32_t active = 0, n = n0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        c[q] = factor[n];
+        wd[q] = __fmul_rn(a.decay, wd[q]);
+        if (!(c[q] < 0.f)) active |= 1u << q;
+        if (++n == N) n = 0;
+    }
+    o.finish(a, element, c, wd, mask, active);
+}
+
+template <class TW, class TG, int RULE>
+static cudaError_t launch_rule(const StepArgs &args, cudaStream_t stream)
+{
+    const uint32_t units = args.pop.n_groups / 2, per_chunk = chunk_units(args.pop.layout, args.pop.N);
+    const uint64_t chunks = (units + per_chunk - 1) / per_chunk, grid = args.pop.layout == kLayoutNP ? chunks * args.pop.N : chunks;
+    if (grid > 0x7FFFFFFFull) return cudaErrorInvalidConfiguration;
+    if (args.pop.layout == kLayoutNP) return launch_chained(step_np_kernel<TW, TG, RULE>, static_cast<unsigned>(grid), kChunkThreads, 0, stream, args);
+    return launch_chained(step_pn_kernel<TW, TG, RULE>, static_cast<unsigned>(grid), kChunkThreads, 0, stream, args);
+}
+
+template <class TW, class TG>
+static cudaError_t launch_typed(const StepArgs &args, int rule, cudaStream_t stream)
+{
+    switch (rule) {
+    case kRuleSgd: return launch_rule<TW, TG, kRuleSgd>(args, stream);
+    case kRuleMomentum: return launch_rule<TW, TG, kRuleMomentum>(args, stream);
+    case kRuleNesterov: return launch_rule<TW, TG, kRuleNesterov>(args, stream);
+    default: return launch_rule<TW, TG, kRuleAdamW>(args, stream);
+    }
+}
+
+cudaError_t launch_step(const StepArgs &args, int rule, int params_dtype, int grads_dtype, cudaStream_t stream)
+{
+    if (params_dtype == kDtypeF32) return grads_dtype == kDtypeF32 ? launch_typed<F32, F32>(args, rule, stream) : launch_typed<F32, BF16>(args, rule, stream);
+    return grads_dtype == kDtypeF32 ? launch_typed<BF16, F32>(args, rule, stream) : launch_typed<BF16, BF16>(args, rule, stream);
+}
+
+}  // namespace wash
