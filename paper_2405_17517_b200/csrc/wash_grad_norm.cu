@@ -2,7 +2,8 @@
 // value is exact there and neither overflows nor underflows), added in an order that depends on the launch's shape only.
 //
 // One pass: a resident grid walks the chunks, a thread adds up its octets' squares, a block leaves one partial sum a model, and the block that reports last
-// adds the blocks' partials and takes the root.
+// adds the blocks' partials and takes the root.  [N][P]: a block has one model, four of 256 threads an SM.  [P][N]: a block has them all, and there is one of 512 threads on
+// an SM, so that the last block has few partial sums to add (N = 64: 444 blocks' took it 10 us).
 #include "wash_octet.cuh"
 
 namespace wash {
@@ -14,11 +15,63 @@ __device__ __forceinline__ double warp_sum(double x)
     return x;
 }
 
-// The block that reports last sums the partials, a warp a model, and leaves the ticket at 0.
-__device__ __forceinline__ void finish_norms(const NormArgs &a)
+// The square of a number in binary64, added to `sum`, without a conversion: those run at a fraction of the rate of multiplications (bf16, [N][P],
+// ResNet-50 N = 8: 129 us with conversions, 76 without).  The pattern of a magnitude, shifted left by 29, is the number times 2^-896 in binary64, denormals
+// included.  Infinities and NaNs come out as numbers of 2^128 and more, so that a sum below 2^256 has none (kSuspect).
+__device__ __forceinline__ double add_square(uint32_t hi, uint32_t lo, double sum)
+{
+    const double x = __hiloint2double(static_cast<int>(hi), static_cast<int>(lo)) * 0x1p896;
+    return fma(x, x, sum);
+}
+constexpr double kSuspect = 0x1p256;
+
+// value q of the octet
+template <class T>
+__device__ __forceinline__ double add_value(const Octet<T> &g, int q, double sum)
+{
+    if constexpr (T::kBytes == 4) {
+        const uint32_t w = g.word(q);
+        return add_square((w >> 3) & 0x0FFFFFFFu, w << 29, sum);
+    } else {
+        const uint32_t w = g.word(q / 2);
+        return add_square((q & 1 ? w >> 3 : w << 13) & 0x0FFFE000u, 0u, sum);
+    }
+}
+
+// Clears the values of an octet that do not exist.
+template <class T>
+__device__ __forceinline__ void keep_existing(Octet<T> &g, uint32_t mask)
+{
+    Octet<T> zero;
+#pragma unroll
+    for (int i = 0; i < Octet<T>::kVecs; ++i) zero.v[i] = make_uint4(0u, 0u, 0u, 0u);
+    g.merge(zero, mask);
+}
+
+// A sum of kSuspect and more: are there infinities or NaNs among the octet's values?  bit 0, bit 1 of value q's two bits.
+template <class T>
+__device__ __forceinline__ uint32_t specials(const Octet<T> &g)
+{
+    uint32_t found = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        const uint32_t magnitude = __float_as_uint(g.get(q)) & 0x7FFFFFFFu;
+        found |= (magnitude > 0x7F800000u ? 2u : magnitude == 0x7F800000u ? 1u : 0u) << (2 * q);
+    }
+    return found;
+}
+__device__ __forceinline__ double with_specials(double sum, uint32_t found)
+{
+    return found & 2u ? __longlong_as_double(0x7FF8000000000000ll) : found & 1u ? __longlong_as_double(0x7FF0000000000000ll) : sum;
+}
+
+// The blocks' partial sums lie one block after the other, N to a block.  The block that reports last adds them up and leaves the ticket at 0: thread t takes
+// every (THREADS / N * N)-th from t on, all of model t mod N, then the threads of a model are added up.
+template <int THREADS>
+__device__ __forceinline__ void finish_norms(const NormArgs &a, double *part)
 {
     __shared__ bool last;
-    __syncthreads();   // the block's partials are stored
+    __syncthreads();   // the block's partials are stored, `part` is free
     if (threadIdx.x == 0) {
         __threadfence();
         last = atomicInc(a.ticket, gridDim.x - 1u) == gridDim.x - 1u;
@@ -26,104 +79,178 @@ __device__ __forceinline__ void finish_norms(const NormArgs &a)
     }
     __syncthreads();
     if (!last) return;
+    const uint32_t N = static_cast<uint32_t>(a.pop.N), shares = THREADS / N, stride = shares * N, count = a.per_model * N;
+    double s = 0.0;
+    if (threadIdx.x < stride) {
+        constexpr int kBatch = 16;   // loads in flight: a trip to the L2 is most of this kernel's end
+        for (uint32_t i = threadIdx.x; i < count; i += kBatch * stride) {
+            double v[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) v[k] = i + k * stride < count ? __ldcg(a.partial + i + k * stride) : 0.0;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) s += v[k];
+        }
+    }
+    part[threadIdx.x] = s;   // of model threadIdx.x mod N
+    __syncthreads();
     const uint32_t lane = threadIdx.x & 31u;
-    for (int n = static_cast<int>(threadIdx.x >> 5); n < a.pop.N; n += kChunkThreads / 32) {
-        double s = 0.0;
-        for (uint32_t b = lane; b < a.per_model; b += 32) s += __ldcg(a.partial + static_cast<size_t>(n) * a.per_model + b);
-        s = warp_sum(s);
-        if (lane == 0) a.out[n] = sqrt(s);
+    for (uint32_t n = threadIdx.x >> 5; n < N; n += THREADS / 32) {
+        double sum = 0.0;
+        for (uint32_t i = lane; i < shares; i += 32) sum += part[i * N + n];
+        sum = warp_sum(sum);
+        if (lane == 0) a.out[n] = sqrt(sum);
     }
 }
 
+// Where a block's value f lies in shared memory: eight neighbours trade places, so that neither the threads' writes (8 values apart) nor the reads of a model's
+// values (N apart) fall into one bank (N = 64, 10408 coordinates: 13 us without).
+__device__ __forceinline__ uint32_t spread(uint32_t f) { return (f & ~7u) | ((f ^ (f >> 3) ^ (f >> 6)) & 7u); }
+
+constexpr int kNormThreadsNP = 256, kNormThreadsPN = 512;
+// Octets a thread has in flight: 64 bytes.
 template <class T>
-__global__ void __launch_bounds__(kChunkThreads) norm_np_kernel(const __grid_constant__ NormArgs a)
+constexpr int kTogether = 64 / (8 * T::kBytes);
+
+template <class T>
+__global__ void __launch_bounds__(kNormThreadsNP, norm_blocks_np(T::kCode)) norm_np_kernel(const __grid_constant__ NormArgs a)
 {
     await_previous();
     let_next_start();
-    const uint32_t n = blockIdx.x / a.per_model, b = blockIdx.x - n * a.per_model;
+    constexpr int K = kTogether<T>;
+    __shared__ double part[kNormThreadsNP];
+    const uint32_t N = static_cast<uint32_t>(a.pop.N), b = blockIdx.x / N, n = blockIdx.x - b * N, lane = threadIdx.x & 31u;
     const char *row = static_cast<const char *>(a.grads) + static_cast<size_t>(n) * a.pop.padded_P * T::kBytes;
-    double sum = 0.0;
-    for (uint32_t c = b; c < a.n_chunks; c += a.per_model) {
-        const uint32_t unit = a.unit_lo + c * kChunkThreads + threadIdx.x;
-        if (unit >= a.unit_hi) break;
-        Octet<T> g;
-        g.load(row + static_cast<size_t>(unit) * 8 * T::kBytes);
-        float decay;
-        const uint32_t mask = existing_np(a.pop, 8ll * unit, a.status, &decay);
+    double sum[4] = {0.0, 0.0, 0.0, 0.0};
+    Place at = {0, 0, 0, 0, 0.f};
+    const auto load = [&](Octet<T> &g, uint32_t unit) {
+        if (unit < a.unit_hi) g.load(row + static_cast<size_t>(unit) * 8 * T::kBytes);
+        else keep_existing(g, 0u);
+    };
+    for (uint32_t c = b * K; c < a.n_chunks; c += a.per_model * K) {
+        const uint32_t first = a.unit_lo + c * kNormThreadsNP, unit = first + threadIdx.x;
+        Octet<T> g[K];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const double x = (mask >> q) & 1u ? static_cast<double>(g.get(q)) : 0.0;
-            sum = fma(x, x, sum);
+        for (int k = 0; k < K; ++k) load(g[k], unit + k * kNormThreadsNP);
+        if (!one_tensor(a.pop, at, 8ll * first, K * kNormThreadsNP * 8, a.status)) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float decay;
+                if (unit + k * kNormThreadsNP < a.unit_hi) keep_existing(g[k], existing_np(a.pop, 8ll * (unit + k * kNormThreadsNP), a.status, &decay));
+            }
         }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q % 4] = add_value(g[k], q, sum[q % 4]);
     }
-    __shared__ double part[kChunkThreads / 32];
-    sum = warp_sum(sum);
-    if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = sum;
+    double total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    if (total >= kSuspect) {   // large, or not numbers: look again
+        uint32_t found = 0;
+        for (uint32_t c = b * K; c < a.n_chunks; c += a.per_model * K)
+            for (int k = 0; k < K; ++k) {
+                const uint32_t unit = a.unit_lo + (c + k) * kNormThreadsNP + threadIdx.x;
+                if (unit >= a.unit_hi) continue;
+                Octet<T> g;
+                float decay;
+                load(g, unit);
+                keep_existing(g, existing_np(a.pop, 8ll * unit, a.status, &decay));
+                found |= specials(g);
+            }
+        found |= found >> 8;
+        found |= found >> 4;
+        total = with_specials(total, found | found >> 2);
+    }
+    total = warp_sum(total);
+    if (lane == 0) part[threadIdx.x >> 5] = total;
     __syncthreads();
     if (threadIdx.x == 0) {
         double s = 0.0;
 #pragma unroll
-        for (int w = 0; w < kChunkThreads / 32; ++w) s += part[w];
-        a.partial[static_cast<size_t>(n) * a.per_model + b] = s;
+        for (int w = 0; w < kNormThreadsNP / 32; ++w) s += part[w];
+        a.partial[blockIdx.x] = s;
     }
-    finish_norms(a);
+    finish_norms<kNormThreadsNP>(a, part);
 }
 
 template <class T>
-__global__ void __launch_bounds__(kChunkThreads) norm_pn_kernel(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(const __grid_constant__ NormArgs a)
 {
     await_previous();
     let_next_start();
-    const uint32_t N = static_cast<uint32_t>(a.pop.N), units = chunk_units(kLayoutPN, a.pop.N), octets = units * N;
+    constexpr int K = kTogether<T>;
+    __shared__ double part[8 * kNormThreadsPN];
+    const uint32_t N = static_cast<uint32_t>(a.pop.N), units = kNormThreadsPN / N, octets = units * N;
     const uint32_t e0 = 8u * threadIdx.x / N, n0 = 8u * threadIdx.x - e0 * N;
     double sum[8];   // of model (n0 + q) mod N
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum[q] = 0.0;
-    for (uint32_t c = blockIdx.x; c < a.n_chunks; c += gridDim.x) {
-        const uint32_t first = a.unit_lo + c * units, here = min(units, a.unit_hi - first) * N;
-        if (threadIdx.x >= here) break;
-        Octet<T> g;
-        g.load(static_cast<const char *>(a.grads) + (static_cast<size_t>(first) * N + threadIdx.x) * 8 * T::kBytes);
-        float decay[8];
-        const uint32_t mask = existing_pn(a.pop, 8ll * first + e0, n0, a.status, decay);
+    Place at = {0, 0, 0, 0, 0.f};
+    // of the chunk whose first unit is `first`
+    const auto there = [&](uint32_t first) { return threadIdx.x < octets && first < a.unit_hi && (units <= a.unit_hi - first || threadIdx.x < (a.unit_hi - first) * N); };
+    const auto load = [&](Octet<T> &g, uint32_t first) {
+        if (there(first)) g.load(static_cast<const char *>(a.grads) + (static_cast<size_t>(first) * N + threadIdx.x) * 8 * T::kBytes);
+        else keep_existing(g, 0u);
+    };
+    for (uint32_t c = blockIdx.x * K; c < a.n_chunks; c += gridDim.x * K) {
+        const uint32_t first = a.unit_lo + c * units;
+        Octet<T> g[K];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const double x = (mask >> q) & 1u ? static_cast<double>(g.get(q)) : 0.0;
-            sum[q] = fma(x, x, sum[q]);
+        for (int k = 0; k < K; ++k) load(g[k], first + k * units);
+        if (!one_tensor(a.pop, at, 8ll * first, K * units * 8, a.status)) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float decay[8];
+                if (there(first + k * units)) keep_existing(g[k], existing_pn(a.pop, 8ll * (first + k * units) + e0, n0, a.status, decay));
+            }
         }
-    }
-    __shared__ double part[8 * kChunkThreads];   // value f of the chunk's 8 * octets: model f mod N
 #pragma unroll
-    for (int q = 0; q < 8; ++q) part[8u * threadIdx.x + q] = sum[q];
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum[q] = add_value(g[k], q, sum[q]);
+    }
+    bool suspect = false;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) suspect = suspect || sum[q] >= kSuspect;
+    if (suspect) {
+        uint32_t found = 0;
+        for (uint32_t c = blockIdx.x * K; c < a.n_chunks; c += gridDim.x * K)
+            for (int k = 0; k < K; ++k) {
+                const uint32_t first = a.unit_lo + (c + k) * units;
+                if (!there(first)) continue;
+                Octet<T> g;
+                float decay[8];
+                load(g, first);
+                keep_existing(g, existing_pn(a.pop, 8ll * first + e0, n0, a.status, decay));
+                found |= specials(g);
+            }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum[q] = with_specials(sum[q], found >> (2 * q));
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) part[spread(8u * threadIdx.x + q)] = sum[q];   // value f of the chunk's 8 * octets: model f mod N
     __syncthreads();
     const uint32_t lane = threadIdx.x & 31u;
-    for (uint32_t n = threadIdx.x >> 5; n < N; n += kChunkThreads / 32) {   // 8 * units values a model
+    for (uint32_t n = threadIdx.x >> 5; n < N; n += kNormThreadsPN / 32) {   // 8 * units values a model
         double s = 0.0;
-        for (uint32_t i = lane; i < 8u * units; i += 32) s += part[i * N + n];
+        for (uint32_t i = lane; i < 8u * units; i += 32) s += part[spread(i * N + n)];
         s = warp_sum(s);
-        if (lane == 0) a.partial[static_cast<size_t>(n) * a.per_model + blockIdx.x] = s;
+        if (lane == 0) a.partial[static_cast<size_t>(blockIdx.x) * N + n] = s;
     }
-    finish_norms(a);
-}
-
-template <class T>
-static cudaError_t launch_typed(const NormArgs &args, uint32_t grid, cudaStream_t stream)
-{
-    if (args.pop.layout == kLayoutNP) return launch_chained(norm_np_kernel<T>, grid, kChunkThreads, 0, stream, args);
-    return launch_chained(norm_pn_kernel<T>, grid, kChunkThreads, 0, stream, args);
+    finish_norms<kNormThreadsPN>(a, part);
 }
 
 cudaError_t launch_grad_norm(NormArgs args, int dtype, int sm_count, cudaStream_t stream)
 {
-    const uint32_t units = args.unit_hi - args.unit_lo, per_chunk = chunk_units(args.pop.layout, args.pop.N);
-    const uint32_t sm = static_cast<uint32_t>(sm_count), N = static_cast<uint32_t>(args.pop.N);
+    const uint32_t units = args.unit_hi - args.unit_lo, sm = static_cast<uint32_t>(sm_count), N = static_cast<uint32_t>(args.pop.N);
+    const bool np = args.pop.layout == kLayoutNP, f32 = dtype == kDtypeF32;
+    const uint32_t per_chunk = np ? kNormThreadsNP : kNormThreadsPN / N;
+    const uint32_t together = f32 ? kTogether<F32> : kTogether<BF16>;
     args.n_chunks = (units + per_chunk - 1) / per_chunk;
-    uint32_t most = args.pop.layout == kLayoutNP ? kNormBlocksNP * sm / N : kNormBlocksPN * sm;
-    if (most < 1) most = 1;
-    args.per_model = args.n_chunks < most ? args.n_chunks : most;
-    if (args.per_model < 1) args.per_model = 1;   // an empty range: one block finds nothing
-    const uint32_t grid = args.pop.layout == kLayoutNP ? args.per_model * N : args.per_model;
-    return dtype == kDtypeF32 ? launch_typed<F32>(args, grid, stream) : launch_typed<BF16>(args, grid, stream);
+    const uint32_t trips = (args.n_chunks + together - 1) / together, most = np ? norm_blocks_np(dtype) * sm / N : kNormBlocksPN * sm;
+    args.per_model = trips < most ? trips : most;
+    if (args.per_model < 1) args.per_model = 1;   // an empty range: a block finds nothing
+    if (np) return launch_chained(f32 ? norm_np_kernel<F32> : norm_np_kernel<BF16>, args.per_model * N, kNormThreadsNP, 0, stream, args);
+    return launch_chained(f32 ? norm_pn_kernel<F32> : norm_pn_kernel<BF16>, args.per_model, kNormThreadsPN, 0, stream, args);
 }
 
 }  // namespace wash

@@ -240,18 +240,19 @@ struct NormArgs {
     const void *grads;
     uint32_t unit_lo, unit_hi;   // units of 8 coordinates to cover
     uint32_t n_chunks;           // chunks they take
-    uint32_t per_model;          // blocks of a model ([N][P]); [P][N]: all blocks, every one of which has a part of every model
-    double *partial;             // [N][per_model]
+    uint32_t per_model;          // blocks of a model ([N][P]: block b is of model b mod N); [P][N]: all blocks, every one of which has a part of every model
+    double *partial;             // [per_model][N]
     uint32_t *ticket;            // blocks that have reported; 0 between launches
     double *out;                 // [N]
     uint32_t *status;
 };
 // Blocks of the norm's grid, and the partial sums they leave.
-constexpr int kNormBlocksNP = 8, kNormBlocksPN = 4;   // an SM
+constexpr int norm_blocks_np(int dtype) { return dtype == kDtypeF32 ? 5 : 4; }   // an SM; five of bf16 have too few registers
+constexpr int kNormBlocksPN = 2;
 inline size_t norm_partials(int layout, int n_models, int sm_count)
 {
     const size_t n = static_cast<size_t>(n_models), sm = static_cast<size_t>(sm_count);
-    return layout == kLayoutNP ? kNormBlocksNP * sm + n : kNormBlocksPN * sm * n;
+    return layout == kLayoutNP ? norm_blocks_np(kDtypeF32) * sm + n : kNormBlocksPN * sm * n;
 }
 
 struct ClipArgs {

@@ -37,21 +37,43 @@ struct Octet {
         if constexpr (T::kBytes == 4) return word(q);
         else return (q & 1) ? word(q / 2) >> 16 : word(q / 2) & 0xFFFFu;
     }
-    // the values of `r` whose bit is set in `active`, the others' bits as they are
-    __device__ __forceinline__ void put(const float (&r)[8], uint32_t active)
+    // The values of `r`, which are results of arithmetic: a NaN among them has the one pattern that the conversion to bf16 gives it, too.
+    __device__ __forceinline__ void put(const float (&r)[8])
     {
         uint32_t w[4 * kVecs];
 #pragma unroll
         for (int i = 0; i < 4 * kVecs; ++i) {
-            if constexpr (T::kBytes == 4) w[i] = (active >> i) & 1u ? __float_as_uint(r[i]) : word(i);
+            if constexpr (T::kBytes == 4) w[i] = __float_as_uint(r[i]);
+            else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(r[2 * i + 1]), "f"(r[2 * i]));
+        }
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+    // the values whose bit is set in `mask` stay, the others become `other`'s
+    __device__ __forceinline__ void merge(const Octet &other, uint32_t mask)
+    {
+        uint32_t w[4 * kVecs];
+#pragma unroll
+        for (int i = 0; i < 4 * kVecs; ++i) {
+            if constexpr (T::kBytes == 4) w[i] = (mask >> i) & 1u ? word(i) : other.word(i);
             else {
-                const uint32_t fresh = BF16::pair_from_floats(r[2 * i], r[2 * i + 1]), two = (active >> (2 * i)) & 3u;
-                const uint32_t mask = (two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u);
-                w[i] = (fresh & mask) | (word(i) & ~mask);
+                const uint32_t two = (mask >> (2 * i)) & 3u, keep = (two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u);
+                w[i] = (word(i) & keep) | (other.word(i) & ~keep);
             }
         }
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+    // the values of `r` whose bit is set in `active`, the others' bits as they are
+    __device__ __forceinline__ void put(const float (&r)[8], uint32_t active)
+    {
+        if (active == 0xFFu) {
+            put(r);
+            return;
+        }
+        const Octet before = *this;
+        put(r);
+        merge(before, active);
     }
     __device__ __forceinline__ void store_some(char *p, uint32_t mask) const
     {
@@ -91,6 +113,13 @@ __device__ __forceinline__ Place find_place(const PopView &pop, long long e, uin
         at.real_end = at.begin;
     }
     return at;
+}
+
+// Whether coordinates [e, e + count) exist and belong to one tensor; `at` is the tensor looked up last.
+__device__ __forceinline__ bool one_tensor(const PopView &pop, Place &at, long long e, uint32_t count, uint32_t *status)
+{
+    if (e < at.begin || e >= at.end) at = find_place(pop, e, status);
+    return e + count <= at.real_end;
 }
 
 // [N][P]: which of the unit's 8 coordinates exist, and their tensor's decay.
