@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksNP) clip_np_kernel(c
     }
     __syncthreads();
     const uint32_t count = count_shared, unit_hi = a.pop.n_groups / 2;
-    Place at = {0, 0, 0, 0, 0.f};
+    Place at = kNowhere;
     for (uint32_t w = blockIdx.x; w < trips * count; w += gridDim.x) {
         const uint32_t trip = w / count, j = w - trip * count, first = (trips - 1u - trip) * K * kChunkThreads, unit = first + threadIdx.x;
         char *row = static_cast<char *>(a.grads) + (static_cast<size_t>(models[j]) * a.pop.padded_P + 8ull * unit) * T::kBytes;
@@ -62,13 +62,13 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksNP) clip_np_kernel(c
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (unit + k * kChunkThreads < unit_hi) g[k].load(row + static_cast<size_t>(k * kChunkThreads) * 8 * T::kBytes);
-        const bool whole = one_tensor(a.pop, at, 8ll * first, K * kChunkThreads * 8, a.status);
+        const bool whole = one_tensor(a.pop, at, first, K * kChunkThreads, a.status);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             if (unit + k * kChunkThreads >= unit_hi) break;
             char *out = row + static_cast<size_t>(k * kChunkThreads) * 8 * T::kBytes;
             float decay;
-            const uint32_t mask = whole ? 0xFFu : existing_np(a.pop, 8ll * (unit + k * kChunkThreads), a.status, &decay);
+            const uint32_t mask = whole ? 0xFFu : existing_np(a.pop, unit + k * kChunkThreads, a.status, &decay);
             scale_octet(g[k], c, 0xFFu);
             if (mask == 0xFFu) g[k].store(out);
             else g[k].store_some(out, mask);
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksPN) clip_pn_kernel(c
         if (++n == N) n = 0;
     }
     if (threadIdx.x >= octets || !active) return;
-    Place at = {0, 0, 0, 0, 0.f};
+    Place at = kNowhere;
     for (uint32_t trip = blockIdx.x; trip < trips; trip += gridDim.x) {
         const uint32_t first = (trips - 1u - trip) * K * units;
         const uint64_t left = static_cast<uint64_t>(unit_hi - first) * N;   // octets from here on
@@ -106,13 +106,13 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksPN) clip_pn_kernel(c
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (k * octets + threadIdx.x < left) g[k].load(src + static_cast<size_t>(k * octets) * 8 * T::kBytes);
-        const bool whole = one_tensor(a.pop, at, 8ll * first, K * units * 8, a.status);
+        const bool whole = one_tensor(a.pop, at, first, K * units, a.status);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             if (k * octets + threadIdx.x >= left) break;
             char *out = src + static_cast<size_t>(k * octets) * 8 * T::kBytes;
             float decay[8];
-            const uint32_t mask = whole ? 0xFFu : existing_pn(a.pop, 8ll * (first + k * units) + e0, n0, a.status, decay);
+            const uint32_t mask = whole ? 0xFFu : existing_pn(a.pop, first + k * units, e0, n0, a.status, decay);
             scale_octet(g[k], c, active);
             if (mask == 0xFFu) g[k].store(out);
             else g[k].store_some(out, mask & active);

@@ -17,6 +17,17 @@ struct Octet {
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) v[i] = F32::load_group(p + 16 * i);
     }
+    // the same for what is not used again soon: it leaves the caches first
+    __device__ __forceinline__ void load_once(const char *p)
+    {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i] = __ldcs(reinterpret_cast<const uint4 *>(p + 16 * i));
+    }
+    __device__ __forceinline__ void store_once(char *p) const
+    {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) __stcs(reinterpret_cast<uint4 *>(p + 16 * i), v[i]);
+    }
     __device__ __forceinline__ void store(char *p) const
     {
 #pragma unroll
@@ -83,73 +94,82 @@ struct Octet {
     }
 };
 
-// The tensor of coordinate e of a row (4 coordinates to a group of the tables).
+// The tensor of a unit of 8 coordinates of a row.  Units are counted in 32 bits (a row has less than 2^30).
 struct Place {
     uint32_t seg;
-    long long begin, real_end, end;   // of the tensor's coordinates in the row; behind real_end comes padding
+    uint32_t begin, full_end, end;   // units: the tensor's, and how far its units are full; behind its coordinates comes padding
+    uint32_t rest;                   // coordinates of unit full_end (0 to 7)
     float decay;
 };
 __device__ __forceinline__ Place place_entry(const PopView &pop, uint32_t s)
 {
-    const uint4 lo = __ldg(reinterpret_cast<const uint4 *>(pop.seg + s));       // begin, end, tensor, cgroup_begin
+    const uint2 lo = __ldg(reinterpret_cast<const uint2 *>(pop.seg + s));       // group_begin, group_end
     const uint2 hi = __ldg(reinterpret_cast<const uint2 *>(pop.seg + s) + 2);   // numel, decay
     Place at;
     at.seg = s;
-    at.begin = 4ll * lo.x;
-    at.real_end = at.begin + hi.x;
-    at.end = 4ll * lo.y;
+    at.begin = lo.x / 2;
+    at.end = lo.y / 2;
+    at.full_end = at.begin + hi.x / 8;
+    at.rest = hi.x % 8;
     at.decay = __uint_as_float(hi.y);
     return at;
 }
-__device__ __forceinline__ Place find_place(const PopView &pop, long long e, uint32_t *status)
+__device__ __forceinline__ Place find_place(const PopView &pop, uint32_t unit, uint32_t *status)
 {
-    const uint32_t g = static_cast<uint32_t>(e >> 2);
+    const uint32_t g = 2 * unit;
     uint32_t s = __ldg(pop.tile_first + (g >> kTileShift));
     const uint32_t last = static_cast<uint32_t>(pop.n_seg) - 1u;
     while (s < last && g >= __ldg(&pop.seg[s].group_end)) ++s;
     Place at = place_entry(pop, s);
-    if (e < at.begin || e >= at.end) {   // table inconsistent with the row: report, touch nothing
+    if (unit < at.begin || unit >= at.end) {   // table inconsistent with the row: report, touch nothing
         if (status) atomicOr(status, 1u);
-        at.real_end = at.begin;
+        at.full_end = at.begin;
+        at.rest = 0;
     }
     return at;
 }
+constexpr Place kNowhere = {0, 0, 0, 0, 0, 0.f};
 
-// Whether coordinates [e, e + count) exist and belong to one tensor; `at` is the tensor looked up last.
-__device__ __forceinline__ bool one_tensor(const PopView &pop, Place &at, long long e, uint32_t count, uint32_t *status)
+// Whether units [unit, unit + count) exist in full and belong to one tensor; `at` is the tensor looked up last.
+__device__ __forceinline__ bool one_tensor(const PopView &pop, Place &at, uint32_t unit, uint32_t count, uint32_t *status)
 {
-    if (e < at.begin || e >= at.end) at = find_place(pop, e, status);
-    return e + count <= at.real_end;
+    if (unit < at.begin || unit >= at.end) at = find_place(pop, unit, status);
+    return unit + count <= at.full_end;
+}
+
+// which of a unit's 8 coordinates exist
+__device__ __forceinline__ uint32_t existing(const Place &at, uint32_t unit)
+{
+    return unit < at.full_end ? 0xFFu : unit == at.full_end ? (1u << at.rest) - 1u : 0u;
 }
 
 // [N][P]: which of the unit's 8 coordinates exist, and their tensor's decay.
-__device__ __forceinline__ uint32_t existing_np(const PopView &pop, long long e, uint32_t *status, float *decay)
+__device__ __forceinline__ uint32_t existing_np(const PopView &pop, uint32_t unit, uint32_t *status, float *decay)
 {
-    const Place at = find_place(pop, e, status);
+    const Place at = find_place(pop, unit, status);
     *decay = at.decay;
-    const long long left = at.real_end - e;
-    return left >= 8 ? 0xFFu : left > 0 ? (1u << left) - 1u : 0u;
+    return existing(at, unit);
 }
 
-// [P][N]: the same for the octet whose first value is model `n`'s of coordinate e.  Its values may belong to more than one tensor.
-__device__ __forceinline__ uint32_t existing_pn(const PopView &pop, long long e, uint32_t n, uint32_t *status, float (&decay)[8])
+// [P][N]: the same for the octet whose first value is model `n`'s of coordinate `c` (0 and up) from the unit's first on.  Its values may belong to more than
+// one unit and tensor.
+__device__ __forceinline__ uint32_t existing_pn(const PopView &pop, uint32_t unit, uint32_t c, uint32_t n, uint32_t *status, float (&decay)[8])
 {
-    Place at = find_place(pop, e, status);
-    const uint32_t N = static_cast<uint32_t>(pop.N);
-    if (e + (n + 7u) / N < at.real_end) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) decay[q] = at.decay;
-        return 0xFFu;
-    }
+    unit += c / 8;
+    c %= 8;
+    Place at = find_place(pop, unit, status);
     uint32_t mask = 0;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-        if (e >= at.end && at.seg + 1u < static_cast<uint32_t>(pop.n_seg)) at = place_entry(pop, at.seg + 1u);
+        if (unit >= at.end && at.seg + 1u < static_cast<uint32_t>(pop.n_seg)) at = place_entry(pop, at.seg + 1u);
         decay[q] = at.decay;
-        if (e >= at.begin && e < at.real_end) mask |= 1u << q;
-        if (++n == N) {
+        mask |= ((existing(at, unit) >> c) & 1u) << q;
+        if (++n == static_cast<uint32_t>(pop.N)) {
             n = 0;
-            ++e;
+            if (++c == 8) {
+                c = 0;
+                ++unit;
+            }
         }
     }
     return mask;

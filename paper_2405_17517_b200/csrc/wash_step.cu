@@ -2,7 +2,14 @@
 //   SGD    d = c g + wd_t p;  m <- mu m + d;  p <- p - lr u,  u = m, with Nesterov d + mu m, without momentum d
 //   AdamW  g' = c g;  m <- b1 m + (1 - b1) g';  v <- b2 v + (1 - b2) g'^2;
 //          p <- p - lr (s1 m / (s2 sqrt(v) + eps) + wd_t p),  s1 = 1 / (1 - b1^t), s2 = 1 / sqrt(1 - b2^t)
-// in binary32, every operation rounded once (explicit _rn intrinsics), bf16 weights rounded to nearest even at the store.
+// in binary32, every operation rounded once (explicit _rn intrinsics), bf16 weights rounded to nearest even at the store: the step costs nothing more than the
+// bytes it moves, so nothing is approximated (quotient and root as the hardware's approximations: AdamW of bf16 weights 716 -> 686 us, fp32 the same).
+//
+// Bound by HBM: one trip a thread, an octet of every stack, all loads in flight before anything else (a lookup of the tensor in front of the barrier costs a
+// tenth).  Blocks of 256 threads go from the last chunk to the first, as wash_clip.cu has it; the norm's pass leaves little in the L2 that lasts until the step
+// has come to it (ResNet-18 N = 5 norm and step: 214 us in the norm's order, 210 in this; loads and stores marked as used once, or with an evict-first policy: the same or slower).
+// ResNet-50, us and share of the measured copy rate: SGD with momentum N = 10 fp32 753 (104 %), N = 8 bf16 428 (102 %), [P][N] N = 8 582 (107 %) and 410 (107 %);
+// AdamW N = 10 fp32 1084 (101 %), N = 8 bf16 682 (101 %), [P][N] N = 8 849 (103 %) and 689 (100 %).
 #include "wash_octet.cuh"
 
 namespace wash {
@@ -49,8 +56,9 @@ struct StepOctet {
         if constexpr (RULE != kRuleSgd) m.load(static_cast<const char *>(a.m) + element * 4);
         if constexpr (RULE == kRuleAdamW) v.load(static_cast<const char *>(a.v) + element * 4);
     }
-    // mask: values that exist; active: values whose model is updated
-    __device__ __forceinline__ void finish(const StepArgs &a, size_t element, const float (&c)[8], const float (&wd)[8], uint32_t mask, uint32_t active)
+    // c(q), wd(q): factor and decay of value q; mask: values that exist; active: values whose model is updated
+    template <class C, class D>
+    __device__ __forceinline__ void finish(const StepArgs &a, size_t element, C c, D wd, uint32_t mask, uint32_t active)
     {
         float rp[8], rm[8], rv[8];
 #pragma unroll
@@ -58,7 +66,7 @@ struct StepOctet {
             rp[q] = p.get(q);
             rm[q] = RULE != kRuleSgd ? m.get(q) : 0.f;
             rv[q] = RULE == kRuleAdamW ? v.get(q) : 0.f;
-            update<RULE>(a, c[q], wd[q], g.get(q), rp[q], rm[q], rv[q]);
+            update<RULE>(a, c(q), wd(q), g.get(q), rp[q], rm[q], rv[q]);
         }
         p.put(rp, active);
         if constexpr (RULE != kRuleSgd) m.put(rm, active);
@@ -77,12 +85,24 @@ struct StepOctet {
     }
 };
 
+// Blocks an SM holds at least, by the registers that are left to a thread then.  us with 1 / 4 / 5 / 6:
+//   [N][P]  AdamW ResNet-50 N = 8 bf16 724 / - / 682 / 876, ResNet-18 N = 5 fp32 252 / - / 243 / 289; the others have more than five of themselves
+//   [P][N]  ResNet-50 N = 8  momentum fp32 582 / 583 / 591 / 661, bf16 439 / 443 / 410 / 415, bf16 and fp32 474 / 470 / 466 / 525;  without fp32 370 / 371 / 348 / 349, bf16
+//           250 / 251 / 250 / 227;  AdamW fp32 933 / 849 / 1463 (spills), bf16 689 / 692 / 1025
 template <class TW, class TG, int RULE>
-__global__ void __launch_bounds__(kChunkThreads) step_np_kernel(const __grid_constant__ StepArgs a)
+constexpr int step_blocks(int layout)
+{
+    constexpr int halves = (TW::kBytes == 2) + (TG::kBytes == 2);
+    if (layout == kLayoutNP) return RULE == kRuleAdamW ? 5 : 1;
+    return RULE == kRuleAdamW ? 4 : RULE == kRuleSgd ? (halves == 2 ? 6 : 5) : halves ? 5 : 4;
+}
+
+template <class TW, class TG, int RULE>
+__global__ void __launch_bounds__(kChunkThreads, step_blocks<TW, TG, RULE>(kLayoutNP)) step_np_kernel(const __grid_constant__ StepArgs a)
 {
     await_previous();
     let_next_start();
-    const uint32_t N = static_cast<uint32_t>(a.pop.N), chunk = blockIdx.x / N, n = blockIdx.x - chunk * N;
+    const uint32_t N = static_cast<uint32_t>(a.pop.N), back = gridDim.x - 1u - blockIdx.x, chunk = back / N, n = back - chunk * N;
     const uint32_t unit = chunk * kChunkThreads + threadIdx.x;
     if (unit >= a.pop.n_groups / 2) return;
     const size_t element = static_cast<size_t>(n) * a.pop.padded_P + 8ull * unit;
@@ -90,42 +110,46 @@ __global__ void __launch_bounds__(kChunkThreads) step_np_kernel(const __grid_con
     o.load(a, element);
     const float factor = step_factor(a, n);
     if (factor < 0.f) return;
-    float c[8], wd[8], decay;
-    const uint32_t mask = existing_np(a.pop, 8ll * unit, a.status, &decay);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        c[q] = factor;
-        wd[q] = __fmul_rn(a.decay, decay);
-    }
-    o.finish(a, element, c, wd, mask, 0xFFu);
+    float decay;
+    const uint32_t mask = existing_np(a.pop, unit, a.status, &decay);
+    decay = __fmul_rn(a.decay, decay);
+    o.finish(a, element, [&](int) { return factor; }, [&](int) { return decay; }, mask, 0xFFu);
 }
 
 template <class TW, class TG, int RULE>
-__global__ void __launch_bounds__(kChunkThreads) step_pn_kernel(const __grid_constant__ StepArgs a)
+__global__ void __launch_bounds__(kChunkThreads, step_blocks<TW, TG, RULE>(kLayoutPN)) step_pn_kernel(const __grid_constant__ StepArgs a)
 {
     await_previous();
     let_next_start();
     const uint32_t N = static_cast<uint32_t>(a.pop.N), units = chunk_units(kLayoutPN, a.pop.N);
-    const uint32_t first = blockIdx.x * units, here = min(units, a.pop.n_groups / 2 - first) * N;
+    const uint32_t first = (gridDim.x - 1u - blockIdx.x) * units, here = min(units, a.pop.n_groups / 2 - first) * N;
     const size_t element = (static_cast<size_t>(first) * N + threadIdx.x) * 8;
     StepOctet<TW, TG, RULE> o;
     if (threadIdx.x < here) o.load(a, element);
-    __shared__ float factor[kMaxN];
-    if (threadIdx.x < N) factor[threadIdx.x] = step_factor(a, threadIdx.x);
+    __shared__ float factors[kMaxN + 8];   // model after model, and once more the first ones, so that an octet's are neighbours
+    if (threadIdx.x < N) {
+        const float c = step_factor(a, threadIdx.x);
+        for (uint32_t i = threadIdx.x; i < N + 8u; i += N) factors[i] = c;
+    }
     __syncthreads();
     if (threadIdx.x >= here) return;
+    const Place at = find_place(a.pop, first, a.status);   // (before the barrier it holds up the block)
     const uint32_t e0 = 8u * threadIdx.x / N, n0 = 8u * threadIdx.x - e0 * N;
-    float c[8], wd[8];
-    const uint32_t mask = existing_pn(a.pop, 8ll * first + e0, n0, a.status, wd);
-    uint32_t active = 0, n = n0;
+    uint32_t active = 0xFFu;
+    if (a.skip_nonfinite) {
+        active = 0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        c[q] = factor[n];
-        wd[q] = __fmul_rn(a.decay, wd[q]);
-        if (!(c[q] < 0.f)) active |= 1u << q;
-        if (++n == N) n = 0;
+        for (int q = 0; q < 8; ++q) active |= factors[n0 + q] < 0.f ? 0u : 1u << q;
     }
-    o.finish(a, element, c, wd, mask, active);
+    const auto c = [&](int q) { return factors[n0 + q]; };
+    if (first + units <= at.full_end) {   // the chunk lies in one tensor
+        const float decay = __fmul_rn(a.decay, at.decay);
+        o.finish(a, element, c, [&](int) { return decay; }, 0xFFu, active);
+    } else {
+        float wd[8];
+        const uint32_t mask = existing_pn(a.pop, first, e0, n0, a.status, wd);
+        o.finish(a, element, c, [&](int q) { return __fmul_rn(a.decay, wd[q]); }, mask, active);
+    }
 }
 
 template <class TW, class TG, int RULE>
