@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksNP) clip_np_kernel(c
     }
     __syncthreads();
     const uint32_t count = count_shared, unit_hi = a.pop.n_groups / 2;
-    Place at = kNowhere;
+    FullUnits full;
     for (uint32_t w = blockIdx.x; w < trips * count; w += gridDim.x) {
         const uint32_t trip = w / count, j = w - trip * count, first = (trips - 1u - trip) * K * kChunkThreads, unit = first + threadIdx.x;
         char *row = static_cast<char *>(a.grads) + (static_cast<size_t>(models[j]) * a.pop.padded_P + 8ull * unit) * T::kBytes;
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksNP) clip_np_kernel(c
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (unit + k * kChunkThreads < unit_hi) g[k].load(row + static_cast<size_t>(k * kChunkThreads) * 8 * T::kBytes);
-        const bool whole = one_tensor(a.pop, at, first, K * kChunkThreads, a.status);
+        const bool whole = one_tensor(a.pop, full, first, K * kChunkThreads, a.status);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             if (unit + k * kChunkThreads >= unit_hi) break;
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksPN) clip_pn_kernel(c
         if (++n == N) n = 0;
     }
     if (threadIdx.x >= octets || !active) return;
-    Place at = kNowhere;
+    FullUnits full;
     for (uint32_t trip = blockIdx.x; trip < trips; trip += gridDim.x) {
         const uint32_t first = (trips - 1u - trip) * K * units;
         const uint64_t left = static_cast<uint64_t>(unit_hi - first) * N;   // octets from here on
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksPN) clip_pn_kernel(c
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (k * octets + threadIdx.x < left) g[k].load(src + static_cast<size_t>(k * octets) * 8 * T::kBytes);
-        const bool whole = one_tensor(a.pop, at, first, K * units, a.status);
+        const bool whole = one_tensor(a.pop, full, first, K * units, a.status);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             if (k * octets + threadIdx.x >= left) break;

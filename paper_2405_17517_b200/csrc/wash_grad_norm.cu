@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kNormThreadsNP, norm_blocks_np(T::kCode)) norm
     const uint32_t N = static_cast<uint32_t>(a.pop.N), b = blockIdx.x / N, n = blockIdx.x - b * N, lane = threadIdx.x & 31u;
     const char *row = static_cast<const char *>(a.grads) + static_cast<size_t>(n) * a.pop.padded_P * T::kBytes;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
-    Place at = kNowhere;
+    FullUnits full;
     const auto load = [&](Octet<T> &g, uint32_t unit) {
         if (unit < a.unit_hi) g.load(row + static_cast<size_t>(unit) * 8 * T::kBytes);
         else keep_existing(g, 0u);
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kNormThreadsNP, norm_blocks_np(T::kCode)) norm
         Octet<T> g[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) load(g[k], unit + k * kNormThreadsNP);
-        if (!one_tensor(a.pop, at, first, K * kNormThreadsNP, a.status)) {
+        if (!one_tensor(a.pop, full, first, K * kNormThreadsNP, a.status)) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 float decay;
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(
     double sum[8];   // of model (n0 + q) mod N
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum[q] = 0.0;
-    Place at = kNowhere;
+    FullUnits full;
     // of the chunk whose first unit is `first`
     const auto there = [&](uint32_t first) { return threadIdx.x < octets && first < a.unit_hi && (units <= a.unit_hi - first || threadIdx.x < (a.unit_hi - first) * N); };
     const auto load = [&](Octet<T> &g, uint32_t first) {
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(
         Octet<T> g[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) load(g[k], first + k * units);
-        if (!one_tensor(a.pop, at, first, K * units, a.status)) {
+        if (!one_tensor(a.pop, full, first, K * units, a.status)) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 float decay[8];

@@ -128,13 +128,18 @@ __device__ __forceinline__ Place find_place(const PopView &pop, uint32_t unit, u
     }
     return at;
 }
-constexpr Place kNowhere = {0, 0, 0, 0, 0, 0.f};
-
-// Whether units [unit, unit + count) exist in full and belong to one tensor; `at` is the tensor looked up last.
-__device__ __forceinline__ bool one_tensor(const PopView &pop, Place &at, uint32_t unit, uint32_t count, uint32_t *status)
+// Whether units [unit, unit + count) exist in full and belong to one tensor; `full` is where the tensor looked up last does.
+struct FullUnits {
+    uint32_t begin = 0, end = 0;
+};
+__device__ __forceinline__ bool one_tensor(const PopView &pop, FullUnits &full, uint32_t unit, uint32_t count, uint32_t *status)
 {
-    if (unit < at.begin || unit >= at.end) at = find_place(pop, unit, status);
-    return unit + count <= at.full_end;
+    if (unit < full.begin || unit + count > full.end) {
+        const Place at = find_place(pop, unit, status);
+        full.begin = at.begin;
+        full.end = at.full_end;
+    }
+    return unit + count <= full.end;
 }
 
 // which of a unit's 8 coordinates exist
@@ -158,6 +163,11 @@ __device__ __forceinline__ uint32_t existing_pn(const PopView &pop, uint32_t uni
     unit += c / 8;
     c %= 8;
     Place at = find_place(pop, unit, status);
+    if (unit + (c + (n + 7u) / static_cast<uint32_t>(pop.N)) / 8u < at.full_end) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) decay[q] = at.decay;
+        return 0xFFu;
+    }
     uint32_t mask = 0;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
