@@ -278,13 +278,14 @@ enum wash_step_flags {
 };
 
 /* One step of SGD on every model, in place on the parameter stack and, with momentum, the optimizer-state stack:
- *     d = c_n g + (weight_decay * decay_t) p;   m <- momentum m + d;   p <- p - lr u
+ *     d = (weight_decay * decay_t) p + c_n g;   m <- momentum m + d;   p <- p - lr u
  * with u = m, with WASH_STEP_NESTEROV u = d + momentum m, and with momentum = 0 u = d (the optimizer-state stack is then
  * neither needed nor touched).  Zeros are the state before the first step.
  *   lr, weight_decay   not negative; momentum in [0,1)
  *   dev_norm           DEVICE array of N doubles: c_n as in wash_clip_grads, with the gradients themselves left as they are;
  *                      NULL: c_n = 1 and max_norm is ignored
- * Evaluated in binary32, every operation rounded once and none fused, in the order written; weights and gradients are fp32 or bf16 (widened
+ * Evaluated in binary32: products that are added to something are fused with the addition (one rounding), every other operation is rounded
+ * once, in the order written; weights and gradients are fp32 or bf16 (widened
  * exactly; new weights rounded to nearest even, so that a change below half a unit in the last place of a bf16 weight is lost: lend an fp32 stack where that
  * matters).  The state must be fp32 (WASH_ERR_UNSUPPORTED otherwise: a moving average in bf16 stops moving).  The stacks must not overlap (WASH_ERR_ARG). */
 int wash_sgd_step(wash_ctx *ctx, double lr, double momentum, double weight_decay, int32_t flags, double max_norm,

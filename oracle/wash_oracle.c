@@ -368,7 +368,7 @@ int wo_consensus_sq(const wo_population *pop, const void *stack, int32_t dtype,
  *   wo_sgd_step    d = c g + wd p;  m <- mu m + d;  p <- p - lr u,  u = m | d + mu m (nesterov) | d (mu = 0)
  *   wo_adamw_step  Loshchilov and Hutter, "Decoupled weight decay regularization", Algorithm 2, with the bias
  *                  correction of Kingma and Ba, "Adam"; t = step + 1
- * binary32, one rounding an operation, in the order written.  decay[s] multiplies the weight decay of segment s.  norm == NULL: nothing
+ * binary32; a product that is added to something is fused with the addition (fmaf), every other operation rounds once.  decay[s] multiplies the weight decay of segment s.  norm == NULL: nothing
  * is clipped; skip: models whose norm is not finite keep everything. */
 int wo_grad_norm(const wo_population *pop, const void *grads, int32_t dtype, int32_t seg_lo, int32_t seg_hi, double *norm)
 {
@@ -427,27 +427,22 @@ static int wo_step(const wo_population *pop, int adamw, int nesterov, uint64_t s
                 const size_t idx = wo_index(pop, n, pop->offset[s] + c);
                 const float p = wo_load(params, p_dtype, idx);
                 const float g = factor * wo_load(grads, g_dtype, idx);
-                const float pull = wd * p;
                 float u;
                 if (adamw) {
-                    const float old1 = b1 * m[idx], new1 = keep1 * g;
-                    m[idx] = old1 + new1;
-                    const float old2 = b2 * v[idx], half = keep2 * g, new2 = half * g;
-                    v[idx] = old2 + new2;
-                    const float root = second * sqrtf(v[idx]), denom = root + eps, top = first * m[idx];
+                    const float new1 = keep1 * g, half = keep2 * g, new2 = half * g;
+                    m[idx] = fmaf(b1, m[idx], new1);
+                    v[idx] = fmaf(b2, v[idx], new2);
+                    const float denom = fmaf(second, sqrtf(v[idx]), eps), top = first * m[idx];
                     const float ratio = top / denom;
-                    u = ratio + pull;
+                    u = fmaf(wd, p, ratio);
                 } else {
-                    u = g + pull;
+                    u = fmaf(wd, p, g);
                     if (hyper[1] > 0.0) {
-                        const float old1 = b1 * m[idx];
-                        m[idx] = old1 + u;
-                        const float ahead = b1 * m[idx];
-                        u = nesterov ? u + ahead : m[idx];
+                        m[idx] = fmaf(b1, m[idx], u);
+                        u = nesterov ? fmaf(b1, m[idx], u) : m[idx];
                     }
                 }
-                const float change = lr * u;
-                wo_store(params, p_dtype, idx, p - change);
+                wo_store(params, p_dtype, idx, fmaf(-lr, u, p));
             }
         }
     }

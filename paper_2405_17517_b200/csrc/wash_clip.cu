@@ -65,10 +65,10 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksNP) clip_np_kernel(c
         const bool whole = one_tensor(a.pop, full, first, K * kChunkThreads, a.status);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (unit + k * kChunkThreads >= unit_hi) break;
             char *out = row + static_cast<size_t>(k * kChunkThreads) * 8 * T::kBytes;
             float decay;
-            const uint32_t mask = whole ? 0xFFu : existing_np(a.pop, unit + k * kChunkThreads, a.status, &decay);
+            const uint32_t mask = whole ? 0xFFu : existing_np(a.pop, min(unit + k * kChunkThreads, unit_hi - 1u), a.status, &decay);
+            if (unit + k * kChunkThreads >= unit_hi) continue;
             scale_octet(g[k], c, 0xFFu);
             if (mask == 0xFFu) g[k].store(out);
             else g[k].store_some(out, mask);
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksPN) clip_pn_kernel(c
         if (c[q] != 1.f) active |= 1u << q;
         if (++n == N) n = 0;
     }
-    if (threadIdx.x >= octets || !active) return;
+    if (!__syncthreads_or(threadIdx.x < octets && active)) return;
     FullUnits full;
     for (uint32_t trip = blockIdx.x; trip < trips; trip += gridDim.x) {
         const uint32_t first = (trips - 1u - trip) * K * units;
@@ -105,14 +105,14 @@ __global__ void __launch_bounds__(kChunkThreads, kClipBlocksPN) clip_pn_kernel(c
         Octet<T> g[K];
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (k * octets + threadIdx.x < left) g[k].load(src + static_cast<size_t>(k * octets) * 8 * T::kBytes);
+            if (threadIdx.x < octets && k * octets + threadIdx.x < left && active) g[k].load(src + static_cast<size_t>(k * octets) * 8 * T::kBytes);
         const bool whole = one_tensor(a.pop, full, first, K * units, a.status);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (k * octets + threadIdx.x >= left) break;
             char *out = src + static_cast<size_t>(k * octets) * 8 * T::kBytes;
             float decay[8];
-            const uint32_t mask = whole ? 0xFFu : existing_pn(a.pop, first + k * units, e0, n0, a.status, decay);
+            const uint32_t mask = whole ? 0xFFu : existing_pn(a.pop, first + k * units, e0, n0, unit_hi, a.status, decay);
+            if (threadIdx.x >= octets || k * octets + threadIdx.x >= left || !active) continue;
             scale_octet(g[k], c, active);
             if (mask == 0xFFu) g[k].store(out);
             else g[k].store_some(out, mask & active);

@@ -111,13 +111,13 @@ constexpr int kNormThreadsNP = 256, kNormThreadsPN = 512;
 template <class T>
 constexpr int kTogether = 64 / (8 * T::kBytes);
 
-template <class T>
-__global__ void __launch_bounds__(kNormThreadsNP, norm_blocks_np(T::kCode)) norm_np_kernel(const __grid_constant__ NormArgs a)
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == kNormThreadsNP ? norm_blocks_np(T::kCode) : 1) norm_np_kernel(const __grid_constant__ NormArgs a)
 {
     await_previous();
     let_next_start();
     constexpr int K = kTogether<T>;
-    __shared__ double part[kNormThreadsNP];
+    __shared__ double part[THREADS];
     const uint32_t N = static_cast<uint32_t>(a.pop.N), b = blockIdx.x / N, n = blockIdx.x - b * N, lane = threadIdx.x & 31u;
     const char *row = static_cast<const char *>(a.grads) + static_cast<size_t>(n) * a.pop.padded_P * T::kBytes;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
@@ -127,15 +127,15 @@ __global__ void __launch_bounds__(kNormThreadsNP, norm_blocks_np(T::kCode)) norm
         else keep_existing(g, 0u);
     };
     for (uint32_t c = b * K; c < a.n_chunks; c += a.per_model * K) {
-        const uint32_t first = a.unit_lo + c * kNormThreadsNP, unit = first + threadIdx.x;
+        const uint32_t first = a.unit_lo + c * THREADS, unit = first + threadIdx.x;
         Octet<T> g[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) load(g[k], unit + k * kNormThreadsNP);
-        if (!one_tensor(a.pop, full, first, K * kNormThreadsNP, a.status)) {
+        for (int k = 0; k < K; ++k) load(g[k], unit + k * THREADS);
+        if (!one_tensor(a.pop, full, first, K * THREADS, a.status)) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float decay;
-                if (unit + k * kNormThreadsNP < a.unit_hi) keep_existing(g[k], existing_np(a.pop, unit + k * kNormThreadsNP, a.status, &decay));
+                float decay;   // (values behind unit_hi are zeros)
+                keep_existing(g[k], existing_np(a.pop, min(unit + k * THREADS, a.unit_hi - 1u), a.status, &decay));
             }
         }
 #pragma unroll
@@ -148,12 +148,11 @@ __global__ void __launch_bounds__(kNormThreadsNP, norm_blocks_np(T::kCode)) norm
         uint32_t found = 0;
         for (uint32_t c = b * K; c < a.n_chunks; c += a.per_model * K)
             for (int k = 0; k < K; ++k) {
-                const uint32_t unit = a.unit_lo + (c + k) * kNormThreadsNP + threadIdx.x;
+                const uint32_t unit = a.unit_lo + (c + k) * THREADS + threadIdx.x;
                 if (unit >= a.unit_hi) continue;
                 Octet<T> g;
-                float decay;
                 load(g, unit);
-                keep_existing(g, existing_np(a.pop, unit, a.status, &decay));
+                keep_existing(g, existing(find_place(a.pop, unit, a.status), unit));
                 found |= specials(g);
             }
         found |= found >> 8;
@@ -166,10 +165,11 @@ __global__ void __launch_bounds__(kNormThreadsNP, norm_blocks_np(T::kCode)) norm
     if (threadIdx.x == 0) {
         double s = 0.0;
 #pragma unroll
-        for (int w = 0; w < kNormThreadsNP / 32; ++w) s += part[w];
-        a.partial[blockIdx.x] = s;
+        for (int w = 0; w < THREADS / 32; ++w) s += part[w];
+        if (a.per_model == 1) a.out[n] = sqrt(s);
+        else a.partial[blockIdx.x] = s;
     }
-    finish_norms<kNormThreadsNP>(a, part);
+    if (a.per_model != 1) finish_norms<THREADS>(a, part);
 }
 
 template <class T>
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 float decay[8];
-                if (there(first + k * units)) keep_existing(g[k], existing_pn(a.pop, first + k * units, e0, n0, a.status, decay));
+                keep_existing(g[k], existing_pn(a.pop, first + k * units, e0, n0, a.unit_hi, a.status, decay));
             }
         }
 #pragma unroll
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(
                 Octet<T> g;
                 float decay[8];
                 load(g, first);
-                keep_existing(g, existing_pn(a.pop, first, e0, n0, a.status, decay));
+                keep_existing(g, existing_pn<false>(a.pop, first, e0, n0, a.unit_hi, a.status, decay));
                 found |= specials(g);
             }
 #pragma unroll
@@ -234,22 +234,32 @@ __global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(
         double s = 0.0;
         for (uint32_t i = lane; i < 8u * units; i += 32) s += part[spread(i * N + n)];
         s = warp_sum(s);
-        if (lane == 0) a.partial[static_cast<size_t>(blockIdx.x) * N + n] = s;
+        if (lane == 0 && gridDim.x == 1) a.out[n] = sqrt(s);
+        else if (lane == 0) a.partial[static_cast<size_t>(blockIdx.x) * N + n] = s;
     }
-    finish_norms<kNormThreadsPN>(a, part);
+    if (gridDim.x != 1) finish_norms<kNormThreadsPN>(a, part);
 }
+
+// A small row is not shared out: the blocks' report and the last one's summation take 2 us.  [N][P], fp32, us by coordinates, shared / one block of 256 / of 1024 threads:
+// N = 2 4000 4.2 / 2.2 / 3.1, 10000 4.2 / - / 3.5, 20000 4.2 / - / 4.4;  N = 64 10000 6.5 / - / 3.6, 20000 6.6 / - / 4.5, 40000 7.5 / - / 5.3, 80000 8.6 / - / 6.6 (bf16 9.8 / - / 7.2), 160000 10.5 / - /
+// 9.5;  N = 16 40000 5.0 / - / 5.2.  [P][N], one block of 512: up to four trips (N = 5, 4000 coordinates 5.4 / 4.5).
+constexpr int kAloneThreads = 1024;
+constexpr uint32_t kAloneTripsPN = 4;
+inline uint32_t alone_trips_np(int n_models) { return n_models >= 48 ? 8u : n_models >= 16 ? 2u : 1u; }
 
 cudaError_t launch_grad_norm(NormArgs args, int dtype, int sm_count, cudaStream_t stream)
 {
     const uint32_t units = args.unit_hi - args.unit_lo, sm = static_cast<uint32_t>(sm_count), N = static_cast<uint32_t>(args.pop.N);
     const bool np = args.pop.layout == kLayoutNP, f32 = dtype == kDtypeF32;
-    const uint32_t per_chunk = np ? kNormThreadsNP : kNormThreadsPN / N;
     const uint32_t together = f32 ? kTogether<F32> : kTogether<BF16>;
+    const bool alone = np && units > kNormThreadsNP * together && units <= alone_trips_np(args.pop.N) * kAloneThreads * together;
+    const uint32_t per_chunk = np ? (alone ? kAloneThreads : kNormThreadsNP) : kNormThreadsPN / N;
     args.n_chunks = (units + per_chunk - 1) / per_chunk;
     const uint32_t trips = (args.n_chunks + together - 1) / together, most = np ? norm_blocks_np(dtype) * sm / N : kNormBlocksPN * sm;
     args.per_model = trips < most ? trips : most;
-    if (args.per_model < 1) args.per_model = 1;   // an empty range: a block finds nothing
-    if (np) return launch_chained(f32 ? norm_np_kernel<F32> : norm_np_kernel<BF16>, args.per_model * N, kNormThreadsNP, 0, stream, args);
+    if (args.per_model < 1 || alone || (!np && trips <= kAloneTripsPN)) args.per_model = 1;   // an empty range: a block finds nothing
+    if (alone) return launch_chained(f32 ? norm_np_kernel<F32, kAloneThreads> : norm_np_kernel<BF16, kAloneThreads>, N, kAloneThreads, 0, stream, args);
+    if (np) return launch_chained(f32 ? norm_np_kernel<F32, kNormThreadsNP> : norm_np_kernel<BF16, kNormThreadsNP>, args.per_model * N, kNormThreadsNP, 0, stream, args);
     return launch_chained(f32 ? norm_pn_kernel<F32> : norm_pn_kernel<BF16>, args.per_model, kNormThreadsPN, 0, stream, args);
 }
 

@@ -2,7 +2,7 @@
 //   SGD    d = c g + wd_t p;  m <- mu m + d;  p <- p - lr u,  u = m, with Nesterov d + mu m, without momentum d
 //   AdamW  g' = c g;  m <- b1 m + (1 - b1) g';  v <- b2 v + (1 - b2) g'^2;
 //          p <- p - lr (s1 m / (s2 sqrt(v) + eps) + wd_t p),  s1 = 1 / (1 - b1^t), s2 = 1 / sqrt(1 - b2^t)
-// in binary32, every operation rounded once (explicit _rn intrinsics), bf16 weights rounded to nearest even at the store: the step costs nothing more than the
+// in binary32, products fused with the additions behind them (explicit _rn intrinsics), bf16 weights rounded to nearest even at the store: the step costs nothing more than the
 // bytes it moves, so nothing is approximated (quotient and root as the hardware's approximations: AdamW of bf16 weights 716 -> 686 us, fp32 the same).
 //
 // Bound by HBM: one trip a thread, an octet of every stack, all loads in flight before anything else (a lookup of the tensor in front of the barrier costs a
@@ -18,21 +18,20 @@ template <int RULE>
 __device__ __forceinline__ void update(const StepArgs &a, float c, float wd, float g, float &p, float &m, float &v)
 {
     g = __fmul_rn(c, g);
-    const float pull = __fmul_rn(wd, p);
+    float u;
     if constexpr (RULE == kRuleAdamW) {
-        m = __fadd_rn(__fmul_rn(a.beta1, m), __fmul_rn(a.one_minus_beta1, g));
-        v = __fadd_rn(__fmul_rn(a.beta2, v), __fmul_rn(__fmul_rn(a.one_minus_beta2, g), g));
-        const float denom = __fadd_rn(__fmul_rn(a.second_scale, __fsqrt_rn(v)), a.eps);
-        const float u = __fdiv_rn(__fmul_rn(a.first_scale, m), denom);
-        p = __fsub_rn(p, __fmul_rn(a.lr, __fadd_rn(u, pull)));
+        m = __fmaf_rn(a.beta1, m, __fmul_rn(a.one_minus_beta1, g));
+        v = __fmaf_rn(a.beta2, v, __fmul_rn(__fmul_rn(a.one_minus_beta2, g), g));
+        u = __fdiv_rn(__fmul_rn(a.first_scale, m), __fmaf_rn(a.second_scale, __fsqrt_rn(v), a.eps));
+        u = __fmaf_rn(wd, p, u);
     } else {
-        float u = __fadd_rn(g, pull);
+        u = __fmaf_rn(wd, p, g);
         if constexpr (RULE != kRuleSgd) {
-            m = __fadd_rn(__fmul_rn(a.beta1, m), u);
-            u = RULE == kRuleNesterov ? __fadd_rn(u, __fmul_rn(a.beta1, m)) : m;
+            m = __fmaf_rn(a.beta1, m, u);
+            u = RULE == kRuleNesterov ? __fmaf_rn(a.beta1, m, u) : m;
         }
-        p = __fsub_rn(p, __fmul_rn(a.lr, u));
     }
+    p = __fmaf_rn(-a.lr, u, p);
 }
 
 // A model's factor for a step: -1 (no factor is negative) where the model is to keep everything.
@@ -86,14 +85,15 @@ struct StepOctet {
 };
 
 // Blocks an SM holds at least, by the registers that are left to a thread then.  us with 1 / 4 / 5 / 6:
-//   [N][P]  AdamW ResNet-50 N = 8 bf16 724 / - / 682 / 876, ResNet-18 N = 5 fp32 252 / - / 243 / 289; the others have more than five of themselves
+//   [N][P], 1 / 5 / 6 / 7  ResNet-50 N = 10 fp32 without momentum 467 / 463 / 464 / 446, with 760 / 757 / 767 / 938, AdamW 1082 / 1087 / 1186 / 1618;
+//           N = 8 bf16 243 / 243 / 255 / 220, 440 / 434 / 434 / 436, 699 / 678 / 710 / 852
 //   [P][N]  ResNet-50 N = 8  momentum fp32 582 / 583 / 591 / 661, bf16 439 / 443 / 410 / 415, bf16 and fp32 474 / 470 / 466 / 525;  without fp32 370 / 371 / 348 / 349, bf16
 //           250 / 251 / 250 / 227;  AdamW fp32 933 / 849 / 1463 (spills), bf16 689 / 692 / 1025
 template <class TW, class TG, int RULE>
 constexpr int step_blocks(int layout)
 {
     constexpr int halves = (TW::kBytes == 2) + (TG::kBytes == 2);
-    if (layout == kLayoutNP) return RULE == kRuleAdamW ? 5 : 1;
+    if (layout == kLayoutNP) return RULE == kRuleSgd ? 7 : 5;
     return RULE == kRuleAdamW ? 4 : RULE == kRuleSgd ? (halves == 2 ? 6 : 5) : halves ? 5 : 4;
 }
 
@@ -104,14 +104,14 @@ __global__ void __launch_bounds__(kChunkThreads, step_blocks<TW, TG, RULE>(kLayo
     let_next_start();
     const uint32_t N = static_cast<uint32_t>(a.pop.N), back = gridDim.x - 1u - blockIdx.x, chunk = back / N, n = back - chunk * N;
     const uint32_t unit = chunk * kChunkThreads + threadIdx.x;
-    if (unit >= a.pop.n_groups / 2) return;
+    const uint32_t unit_hi = a.pop.n_groups / 2;
     const size_t element = static_cast<size_t>(n) * a.pop.padded_P + 8ull * unit;
     StepOctet<TW, TG, RULE> o;
-    o.load(a, element);
-    const float factor = step_factor(a, n);
-    if (factor < 0.f) return;
+    if (unit < unit_hi) o.load(a, element);
     float decay;
-    const uint32_t mask = existing_np(a.pop, unit, a.status, &decay);
+    const uint32_t mask = existing_np(a.pop, min(unit, unit_hi - 1u), a.status, &decay);
+    const float factor = step_factor(a, n);
+    if (factor < 0.f || unit >= unit_hi) return;
     decay = __fmul_rn(a.decay, decay);
     o.finish(a, element, [&](int) { return factor; }, [&](int) { return decay; }, mask, 0xFFu);
 }
@@ -132,8 +132,7 @@ __global__ void __launch_bounds__(kChunkThreads, step_blocks<TW, TG, RULE>(kLayo
         for (uint32_t i = threadIdx.x; i < N + 8u; i += N) factors[i] = c;
     }
     __syncthreads();
-    if (threadIdx.x >= here) return;
-    const Place at = find_place(a.pop, first, a.status);   // (before the barrier it holds up the block)
+    const Place at = warp_place(a.pop, first, a.status);   // (before the barrier it holds up the block)
     const uint32_t e0 = 8u * threadIdx.x / N, n0 = 8u * threadIdx.x - e0 * N;
     uint32_t active = 0xFFu;
     if (a.skip_nonfinite) {
@@ -144,10 +143,12 @@ __global__ void __launch_bounds__(kChunkThreads, step_blocks<TW, TG, RULE>(kLayo
     const auto c = [&](int q) { return factors[n0 + q]; };
     if (first + units <= at.full_end) {   // the chunk lies in one tensor
         const float decay = __fmul_rn(a.decay, at.decay);
+        if (threadIdx.x >= here) return;
         o.finish(a, element, c, [&](int) { return decay; }, 0xFFu, active);
     } else {
         float wd[8];
-        const uint32_t mask = existing_pn(a.pop, first, e0, n0, a.status, wd);
+        const uint32_t mask = existing_pn(a.pop, first, e0, n0, a.pop.n_groups / 2, a.status, wd);
+        if (threadIdx.x >= here) return;
         o.finish(a, element, c, [&](int q) { return __fmul_rn(a.decay, wd[q]); }, mask, active);
     }
 }

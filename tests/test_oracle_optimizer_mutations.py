@@ -10,13 +10,13 @@ MUTATIONS = {
     "factor above one": ("if (c > 1.0) c = 1.0;", ""),
     "factor upside down": ("double c = max_norm / (norm + 1e-6);", "double c = norm / (max_norm + 1e-6);"),
     "decay of the first tensor for all": ("(float)hyper[4] * (float)decay[s];", "(float)hyper[4] * (float)decay[0];"),
-    "momentum weighs the gradient too": ("m[idx] = old1 + u;", "m[idx] = old1 + keep1 * u;"),
-    "nesterov always": ("u = nesterov ? u + ahead : m[idx];", "u = u + ahead;"),
+    "momentum weighs the gradient too": ("m[idx] = fmaf(b1, m[idx], u);", "m[idx] = fmaf(b1, m[idx], keep1 * u);"),
+    "nesterov always": ("u = nesterov ? fmaf(b1, m[idx], u) : m[idx];", "u = fmaf(b1, m[idx], u);"),
     "no bias correction of the first moment": ("top = first * m[idx];", "top = m[idx];"),
     "bias correction a step late": ("(long double)step + 1.0L;", "(long double)step + 2.0L;"),
     "second moment of the unclipped gradient's size": ("new2 = half * g;", "new2 = half;"),
-    "eps inside the root": ("const float root = second * sqrtf(v[idx]), denom = root + eps", "const float root = second * sqrtf(v[idx] + eps), denom = root"),
-    "coupled decay": ("u = ratio + pull;", "u = ratio;"),
+    "eps inside the root": ("denom = fmaf(second, sqrtf(v[idx]), eps)", "denom = second * sqrtf(v[idx] + eps)"),
+    "coupled decay": ("u = fmaf(wd, p, ratio);", "u = ratio;"),
     "skipped models stepped": ("if (skip && norm && !isfinite(norm[n])) continue;", ""),
 }
 
