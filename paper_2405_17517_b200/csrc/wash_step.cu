@@ -86,14 +86,14 @@ struct StepOctet {
 
 // Blocks an SM holds at least, by the registers that are left to a thread then.  us with 1 / 4 / 5 / 6:
 //   [N][P], 1 / 5 / 6 / 7  ResNet-50 N = 10 fp32 without momentum 467 / 463 / 464 / 446, with 760 / 757 / 767 / 938, AdamW 1082 / 1087 / 1186 / 1618;
-//           N = 8 bf16 243 / 243 / 255 / 220, 440 / 434 / 434 / 436, 699 / 678 / 710 / 852
+//           N = 8 bf16 243 / 243 / 255 / 220, 438 / 461 / 437 / 439 (fp32 gradients 522 / 494 / 479 / 538), 699 / 678 / 710 / 852
 //   [P][N]  ResNet-50 N = 8  momentum fp32 582 / 583 / 591 / 661, bf16 439 / 443 / 410 / 415, bf16 and fp32 474 / 470 / 466 / 525;  without fp32 370 / 371 / 348 / 349, bf16
 //           250 / 251 / 250 / 227;  AdamW fp32 933 / 849 / 1463 (spills), bf16 689 / 692 / 1025
 template <class TW, class TG, int RULE>
 constexpr int step_blocks(int layout)
 {
     constexpr int halves = (TW::kBytes == 2) + (TG::kBytes == 2);
-    if (layout == kLayoutNP) return RULE == kRuleSgd ? 7 : 5;
+    if (layout == kLayoutNP) return RULE == kRuleAdamW ? 5 : RULE == kRuleSgd ? 7 : halves ? 6 : 5;
     return RULE == kRuleAdamW ? 4 : RULE == kRuleSgd ? (halves == 2 ? 6 : 5) : halves ? 5 : 4;
 }
 
