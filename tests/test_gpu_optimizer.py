@@ -471,3 +471,96 @@ def test_refusals():
     for call in (B.papa_ema,):                                                            # the population operators keep to weights and first state
         refused(B.WASH_ERR_ARG, call, ctx, B.WASH_STACK_GRADS, 0.5)
     c.close()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+def test_both_moments_follow_their_parameters_through_a_shuffle(layout):
+    """WASH+Opt with Adam: the second moment's own context draws the same mask and permutations."""
+    N = 6
+    c = Training(N, RAGGED, layout, seed=14)
+    moments = B.Population(N, RAGGED, layout, 0)
+    moments.bind(B.WASH_STACK_OPT, c.dev["v"])
+    p_layer = B.wash_layer_probs(len(RAGGED), 0.4)
+    for step in range(3):
+        norm = c.norms().copy()
+        _step(c, "adamw", 0.9, False, step, 1.0, norm)
+        B.wash_shuffle_both(c.gpu.ctx, step, 0.0, p_layer, seed=21)
+        B.wash_shuffle_opt_state(moments.ctx, step, 0.0, p_layer, seed=21)
+        oracle.shuffle(c.ora, c.host["p"], p_layer, seed=21, step=step, stack2=c.host["m"])
+        oracle.shuffle(c.ora, c.host["v"], p_layer, seed=21, step=step)
+        c.assert_equal()
+    moments.close()
+    c.close()
+
+
+@pytest.mark.parametrize("numel", [[1] * 700, [9] * 300 + [2000] + [1] * 50, [8] * 400, [i % 7 + 1 for i in range(150)] + [30011] + [5, 5, 5]])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("N", [2, 3, 16, 37])
+def test_many_tiny_tensors(N, layout, numel):
+    """More tensors to a warp's coordinates, and to a lookup tile, than a lookup fetches at once."""
+    c = Training(N, numel, layout, "f32", "bf16", seed=N, decay=_decay(len(numel)))
+    norm = c.norms().copy()
+    assert np.allclose(norm, oracle.grad_norm(c.ora, c.host["g"]), rtol=(sum(numel) + 4) * 2.0 ** -52, atol=0)
+    T = len(numel)
+    assert np.allclose(c.norms(T // 3, T - 2), oracle.grad_norm(c.ora, c.host["g"], T // 3, T - 2), rtol=(sum(numel) + 4) * 2.0 ** -52, atol=0)
+    c.norm.copy_(torch.from_numpy(norm))
+    bound = float(np.median(norm))
+    _step(c, "sgd", 0.9, True, 0, bound, norm)
+    _step(c, "adamw", 0.9, False, 5, bound, norm)
+    B.wash_clip_grads(c.gpu.ctx, bound, c.norm)
+    oracle.clip_grads(c.ora, c.host["g"], bound, norm)
+    c.assert_equal()
+    c.close()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+def test_rows_of_every_size_near_the_kernels_choices(layout):
+    """Norms at the row lengths where one block, one large block or many take a row, and just beside them."""
+    for dtype in ("f32", "bf16"):
+        for N in (2, 16, 48, 64):
+            for P in (4095, 4096, 4104, 8192, 8200, 16384, 16392, 32768, 32776, 131072, 131080):
+                if N * P > 3_000_000:
+                    continue
+                pop = B.Population(N, [P], layout, 0)
+                g = torch.randn(pop.n_elems, device="cuda", generator=torch.Generator("cuda").manual_seed(P + N)).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+                pop.bind(B.WASH_STACK_GRADS, g)
+                out = torch.zeros(N, dtype=torch.float64, device="cuda")
+                B.wash_grad_norm(pop.ctx, 0, 1, out)
+                rows = (g.view(N, -1)[:, :P] if layout == 0 else g.view(-1, N)[:P].t()).double()
+                assert torch.allclose(out, rows.square().sum(1).sqrt(), rtol=2 * P * 2.0 ** -53, atol=0), (dtype, N, P)
+                pop.close()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+def test_stacks_of_more_than_2_to_the_32_elements(layout):
+    """Offsets beyond 32 bits: 64 models of 2^26 + 5 coordinates, zero but for the row's ends and two places in the middle."""
+    N, P = 64, (1 << 26) + 5
+    pop = B.Population(N, [P], layout, 0)
+    stacks = {"p": torch.zeros(pop.n_elems, dtype=torch.bfloat16, device="cuda"), "g": torch.zeros(pop.n_elems, dtype=torch.bfloat16, device="cuda"),
+              "m": torch.zeros(pop.n_elems, device="cuda")}
+    for role, t in stacks.items():
+        pop.bind(ROLES[role], t)
+
+    def at(role):
+        return stacks[role].view(N, pop.padded_P) if layout == 0 else stacks[role].view(pop.padded_P, N).t()
+
+    places = [0, 1, (1 << 25) + 3, (1 << 26) - 7, P - 2, P - 1]
+    values = torch.arange(1, N + 1, device="cuda", dtype=torch.float32)[:, None] * torch.tensor([1.0, 2.0, 4.0, 8.0, 16.0, 32.0], device="cuda")
+    for k, e in enumerate(places):
+        at("g")[:, e] = values[:, k].to(torch.bfloat16)
+    at("g")[:, P:] = float("nan")                                          # padding
+    norm = torch.zeros(N, dtype=torch.float64, device="cuda")
+    B.wash_grad_norm(pop.ctx, 0, 1, norm)
+    want = torch.stack([at("g")[:, e].double() for e in places]).square().sum(0).sqrt()
+    assert torch.allclose(norm, want, rtol=1e-15, atol=0)
+    B.wash_sgd_step(pop.ctx, 0.5, 0.9)
+    B.wash_clip_grads(pop.ctx, float(want[20]), norm)
+    torch.cuda.synchronize()
+    B.wash_check(pop.ctx)
+    g = values.to(torch.bfloat16).float()
+    factor = torch.clamp(want[20] / (want + 1e-6), max=1.0).float()
+    for k, e in enumerate(places):
+        assert (at("m")[:, e] == g[:, k]).all() and (at("p")[:, e] == (-0.5 * g[:, k]).to(torch.bfloat16)).all()
+        assert (at("g")[:, e] == (g[:, k] * factor).to(torch.bfloat16)).all()
+    assert int((stacks["m"] != 0).sum()) == int((stacks["p"] != 0).sum()) == N * len(places)      # and nothing anywhere else
+    pop.close()
