@@ -564,3 +564,29 @@ def test_stacks_of_more_than_2_to_the_32_elements(layout):
         assert (at("g")[:, e] == (g[:, k] * factor).to(torch.bfloat16)).all()
     assert int((stacks["m"] != 0).sum()) == int((stacks["p"] != 0).sum()) == N * len(places)      # and nothing anywhere else
     pop.close()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("P", [9000, 1_500_007])
+def test_norms_of_extreme_values_in_long_rows(P, dtype, layout):
+    """One infinity, one NaN, one row of the largest finite values and rows of small ones, where blocks walk several chunks."""
+    N = 6
+    g = torch.randn(N, P, device="cuda", generator=torch.Generator("cuda").manual_seed(P)) * 1e-3
+    g[1] = 3.3e38
+    g[2, P // 3] = float("inf")
+    g[3, P - 1] = float("nan")
+    g[4] *= 1e-37
+    g[5, P // 2], g[5, P // 2 + 9] = float("-inf"), float("nan")
+    g = g.to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    pop = B.Population(N, [P], layout, 0)
+    stack = torch.full((N, pop.padded_P), float("inf"), dtype=g.dtype, device="cuda")
+    stack[:, :P] = g
+    stack = (stack if layout == 0 else stack.t()).contiguous().view(-1)
+    pop.bind(B.WASH_STACK_GRADS, stack)
+    out = torch.zeros(N, dtype=torch.float64, device="cuda")
+    B.wash_grad_norm(pop.ctx, 0, 1, out)
+    want = g.double().square().sum(1).sqrt()
+    assert torch.allclose(out[[0, 1, 4]], want[[0, 1, 4]], rtol=2 * P * 2.0 ** -53, atol=0)
+    assert out[2] == float("inf") and out[3].isnan() and out[5].isnan()
+    pop.close()
