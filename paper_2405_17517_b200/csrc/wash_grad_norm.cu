@@ -15,9 +15,10 @@ __device__ __forceinline__ double warp_sum(double x)
     return x;
 }
 
-// The square of a number in binary64, added to `sum`, without a conversion: those run at a fraction of the rate of multiplications (bf16, [N][P],
-// ResNet-50 N = 8: 129 us with conversions, 76 without).  The pattern of a magnitude, shifted left by 29, is the number times 2^-896 in binary64, denormals
-// included.  Infinities and NaNs come out as numbers of 2^128 and more, so that a sum below 2^256 has none (kSuspect).
+// A square is added up in binary64 in one of two ways, turn about, since they load different pipes: by converting the number (one instruction, at a fraction of the
+// others' rate), or by the shifts that make a binary64 number of its pattern -- without its sign, moved left by 29, it is the number times 2^-896, denormals
+// included -- and a multiplication.  bf16, ResNet-50 N = 8: conversions alone 74.7 us, shifts alone 71.6, half and half 67.9 ([P][N] 74.3, 75.1, 70.7); fp32 147 all three.
+// Infinities and NaNs come out of the shifts as numbers of 2^128 and more: a sum below 2^256 has none (kSuspect).
 __device__ __forceinline__ double add_square(uint32_t hi, uint32_t lo, double sum)
 {
     const double x = __hiloint2double(static_cast<int>(hi), static_cast<int>(lo)) * 0x1p896;
@@ -29,13 +30,13 @@ constexpr double kSuspect = 0x1p256;
 template <class T>
 __device__ __forceinline__ double add_value(const Octet<T> &g, int q, double sum)
 {
-    if constexpr (T::kBytes == 4) {
-        const uint32_t w = g.word(q);
-        return add_square((w >> 3) & 0x0FFFFFFFu, w << 29, sum);
-    } else {
-        const uint32_t w = g.word(q / 2);
-        return add_square((q & 1 ? w >> 3 : w << 13) & 0x0FFFE000u, 0u, sum);
+    if (q & 1) {
+        const double x = static_cast<double>(g.get(q));
+        return fma(x, x, sum);
     }
+    const uint32_t w = T::kBytes == 4 ? g.word(q) : g.word(q / 2);
+    if constexpr (T::kBytes == 4) return add_square((w >> 3) & 0x0FFFFFFFu, w << 29, sum);
+    else return add_square((w << 13) & 0x0FFFE000u, 0u, sum);
 }
 
 // Clears the values of an octet that do not exist.
@@ -48,7 +49,7 @@ __device__ __forceinline__ void keep_existing(Octet<T> &g, uint32_t mask)
     g.merge(zero, mask);
 }
 
-// A sum of kSuspect and more: are there infinities or NaNs among the octet's values?  bit 0, bit 1 of value q's two bits.
+// A sum that is not below kSuspect: are there infinities or NaNs among the octet's values?  bit 0, bit 1 of value q's two bits.
 template <class T>
 __device__ __forceinline__ uint32_t specials(const Octet<T> &g)
 {
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormThreadsNP ? norm_bloc
             for (int q = 0; q < 8; ++q) sum[q % 4] = add_value(g[k], q, sum[q % 4]);
     }
     double total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    if (total >= kSuspect) {   // large, or not numbers: look again
+    if (!(total < kSuspect)) {   // large, or not numbers: look again
         uint32_t found = 0;
         for (uint32_t c = b * K; c < a.n_chunks; c += a.per_model * K)
             for (int k = 0; k < K; ++k) {
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(
     }
     bool suspect = false;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) suspect = suspect || sum[q] >= kSuspect;
+    for (int q = 0; q < 8; ++q) suspect = suspect || !(sum[q] < kSuspect);
     if (suspect) {
         uint32_t found = 0;
         for (uint32_t c = blockIdx.x * K; c < a.n_chunks; c += gridDim.x * K)
@@ -248,9 +249,10 @@ __global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(
 
 // A small row is not shared out: the blocks' report and the last one's summation take 2 us.  [N][P], fp32, us by coordinates, shared / one block of 256 / of 1024 threads:
 // N = 2 4000 4.2 / 2.2 / 3.1, 10000 4.2 / - / 3.5, 20000 4.2 / - / 4.4;  N = 64 10000 6.5 / - / 3.6, 20000 6.6 / - / 4.5, 40000 7.5 / - / 5.3, 80000 8.6 / - / 6.6 (bf16 9.8 / - / 7.2), 160000 10.5 / - /
-// 9.5;  N = 16 40000 5.0 / - / 5.2.  [P][N], one block of 512: up to four trips (N = 5, 4000 coordinates 5.4 / 4.5).
+// 9.5;  N = 16 40000 5.0 / - / 5.2.  [P][N], one block of 512: N = 16, 1000 coordinates, two trips 5.7 / 4.0; N = 2, 10000, three 5.5 / 4.6, but
+// N = 3 with 12 tensors, 10400, four 5.9 / 7.2.
 constexpr int kAloneThreads = 1024;
-constexpr uint32_t kAloneTripsPN = 4;
+constexpr uint32_t kAloneTripsPN = 2;
 inline uint32_t alone_trips_np(int n_models) { return n_models >= 48 ? 8u : n_models >= 16 ? 2u : 1u; }
 
 cudaError_t launch_grad_norm(NormArgs args, int dtype, int sm_count, cudaStream_t stream)
