@@ -2,8 +2,10 @@
 // value is exact there and neither overflows nor underflows), added in an order that depends on the launch's shape only.
 //
 // One pass: a resident grid walks the chunks, a thread adds up its octets' squares, a block leaves one partial sum a model, and the block that reports last
-// adds the blocks' partials and takes the root.  [N][P]: a block has one model, four of 256 threads an SM.  [P][N]: a block has them all, and there is one of 512 threads on
-// an SM, so that the last block has few partial sums to add (N = 64: 444 blocks' took it 10 us).
+// adds the blocks' partials and takes the root.  [N][P]: a block has one model, five of 256 threads an SM (four for bf16).  [P][N]: a block has them all, and there are two of 512
+// threads an SM, so that the last block has few partial sums to add.
+// Bound by HBM in fp32 (ResNet-50 N = 10 147 us = 6.95 TB/s, [P][N] N = 8 120 us = 6.8), by issue slots in bf16, whose bytes hold twice the values: 8 instructions a
+// value, .65 an issue slot (N = 8 68 us = 6.0 TB/s, [P][N] 71 = 5.8).
 #include "wash_octet.cuh"
 
 namespace wash {
