@@ -2,8 +2,8 @@
 // value is exact there and neither overflows nor underflows), added in an order that depends on the launch's shape only.
 //
 // One pass: a resident grid walks the chunks, a thread adds up its octets' squares, a block leaves one partial sum a model, and the block that reports last
-// adds the blocks' partials and takes the root.  [N][P]: a block has one model, five of 256 threads an SM (four for bf16).  [P][N]: a block has them all, and there are two of 512
-// threads an SM, so that the last block has few partial sums to add.
+// adds the blocks' partials and takes the root.  [N][P]: a block has one model, five of 256 threads an SM (four for bf16).  [P][N]: a block has them all; there are 1024 threads an SM, in
+// four blocks or two.
 // Bound by HBM in fp32 (ResNet-50 N = 10 147 us = 6.95 TB/s, [P][N] N = 8 120 us = 6.8), by issue slots in bf16, whose bytes hold twice the values: 8 instructions a
 // value, .65 an issue slot (N = 8 68 us = 6.0 TB/s, [P][N] 71 = 5.8).
 #include "wash_octet.cuh"
@@ -118,17 +118,13 @@ __device__ __forceinline__ void finish_norms(const NormArgs &a, double *part)
 // values (N apart) fall into one bank (N = 64, 10408 coordinates: 13 us without).
 __device__ __forceinline__ uint32_t spread(uint32_t f) { return (f & ~7u) | ((f ^ (f >> 3) ^ (f >> 6)) & 7u); }
 
-constexpr int kNormThreadsNP = 256, kNormThreadsPN = 512;
-// Octets a thread has in flight: 64 bytes.
-template <class T>
-constexpr int kTogether = 64 / (8 * T::kBytes);
-
-template <class T, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == kNormThreadsNP ? norm_blocks_np(T::kCode) : 1) norm_np_kernel(const __grid_constant__ NormArgs a)
+constexpr int kNormThreads = 256;
+// K: octets a thread has in flight
+template <class T, int THREADS, int K>
+__global__ void __launch_bounds__(THREADS, THREADS == kNormThreads ? norm_blocks_np(T::kCode) : 1) norm_np_kernel(const __grid_constant__ NormArgs a)
 {
     await_previous();
     let_next_start();
-    constexpr int K = kTogether<T>;
     __shared__ double part[THREADS];
     const uint32_t N = static_cast<uint32_t>(a.pop.N), b = blockIdx.x / N, n = blockIdx.x - b * N, lane = threadIdx.x & 31u;
     const char *row = static_cast<const char *>(a.grads) + static_cast<size_t>(n) * a.pop.padded_P * T::kBytes;
@@ -184,14 +180,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormThreadsNP ? norm_bloc
     if (a.per_model != 1) finish_norms<THREADS>(a, part);
 }
 
-template <class T>
-__global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(const __grid_constant__ NormArgs a)
+template <class T, int THREADS, int K>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) norm_pn_kernel(const __grid_constant__ NormArgs a)
 {
     await_previous();
     let_next_start();
-    constexpr int K = kTogether<T>;
-    __shared__ double part[8 * kNormThreadsPN];
-    const uint32_t N = static_cast<uint32_t>(a.pop.N), units = kNormThreadsPN / N, octets = units * N;
+    __shared__ double part[8 * THREADS];
+    const uint32_t N = static_cast<uint32_t>(a.pop.N), units = THREADS / N, octets = units * N;
     const uint32_t e0 = 8u * threadIdx.x / N, n0 = 8u * threadIdx.x - e0 * N;
     double sum[8];   // of model (n0 + q) mod N
 #pragma unroll
@@ -241,36 +236,73 @@ __global__ void __launch_bounds__(kNormThreadsPN, kNormBlocksPN) norm_pn_kernel(
 #pragma unroll
     for (int q = 0; q < 8; ++q) part[spread(8u * threadIdx.x + q)] = sum[q];   // value f of the chunk's 8 * octets: model f mod N
     __syncthreads();
-    sum_models<kNormThreadsPN>(N, 8u * units, [&](uint32_t i, uint32_t n) { return part[spread(i * N + n)]; },
+    sum_models<THREADS>(N, 8u * units, [&](uint32_t i, uint32_t n) { return part[spread(i * N + n)]; },
         [&](uint32_t n, double total) {
             if (gridDim.x == 1) a.out[n] = sqrt(total);
             else a.partial[static_cast<size_t>(blockIdx.x) * N + n] = total;
         });
-    if (gridDim.x != 1) finish_norms<kNormThreadsPN>(a, part);
+    if (gridDim.x != 1) finish_norms<THREADS>(a, part);
 }
 
-// A small row is not shared out: the blocks' report and the last one's summation take 2 us.  [N][P], fp32, us by coordinates, shared / one block of 256 / of 1024 threads:
-// N = 2 4000 4.2 / 2.2 / 3.1, 10000 4.2 / - / 3.5, 20000 4.2 / - / 4.4;  N = 64 10000 6.5 / - / 3.6, 20000 6.6 / - / 4.5, 40000 7.5 / - / 5.3, 80000 8.6 / - / 6.6 (bf16 9.8 / - / 7.2), 160000 10.5 / - /
-// 9.5;  N = 16 40000 5.0 / - / 5.2.  [P][N], one block of 512: N = 16, 1000 coordinates, two trips 5.7 / 4.0; N = 2, 10000, three 5.5 / 4.6, but
-// N = 3 with 12 tensors, 10400, four 5.9 / 7.2.
+// A small row is not shared out: the blocks' report and the last one's summation take 2 us.  [N][P], us by coordinates, shared / one block of 256 / of 1024 threads:
+// fp32 N = 2 4000 3.8 / 2.2 / 3.0, 10000 3.9 / - / 3.3, 20000 3.9 / - / 4.4;  N = 64 10000 6.5 / - / 3.5, 20000 6.6 / - / 4.4, 40000 7.5 / - / 5.2, 80000 8.6 / - / 6.4 (bf16 9.8 / - / 6.9), 160000
+// 10.5 / - / 9.5;  N = 16 20000 4.2 / - / 4.4, 40000 4.2 / - / 5.2; bf16 N = 2 10000 4.1 / - / 4.5.  [P][N], by values: 8000 4.6 / 3.4, bf16 4.8 / 3.9; 16000 4.5 / 3.8; 20000 bf16 4.7 / 4.6.
 constexpr int kAloneThreads = 1024;
-constexpr uint32_t kAloneTripsPN = 2;
-inline uint32_t alone_trips_np(int n_models) { return n_models >= 48 ? 8u : n_models >= 16 ? 2u : 1u; }
+inline uint32_t alone_trips(int n_models, int bytes) { return n_models >= 48 ? 8u : bytes == 4 ? 1u : 0u; }
+// [P][N]: threads of a block, of which an SM has 1024.  Small blocks start and end sooner, but their partial sums, N a block, take the last one longer.  us with 256 / 512, 1, 3, 10 and 30
+// million values: N = 8 fp32 5.6 7.4 8.9 22.7 / 6.8 7.8 8.6 22.5, bf16 6.1 7.3 9.0 13.6 / 8.9 9.0 10.0 14.5;  N = 16 bf16 6.0 8.0 9.8 14.3 / 8.7 9.2 10.3 14.8;  N = 33 fp32 8.2 9.6 11.7 25.3 / 6.5 8.1 10.0
+// 23.3;  N = 64 fp32 9.8 12.3 13.7 27.2 / 6.7 9.3 10.3 24.2, bf16 7.6 11.9 13.7 18.1 / 8.6 9.6 11.7 16.1.
+constexpr int kManyModels = 16, kNormThreadsMany = 512;
+
+// BYTES of gradients a thread has in flight, THREADS of a block, `blocks` at most for a model ([N][P]) or for all.
+template <class T, int THREADS, int BYTES>
+static cudaError_t launch_norm(NormArgs args, uint32_t blocks, cudaStream_t stream)
+{
+    constexpr int K = BYTES / (8 * T::kBytes);
+    const uint32_t N = static_cast<uint32_t>(args.pop.N), units = args.unit_hi - args.unit_lo;
+    const bool np = args.pop.layout == kLayoutNP;
+    const uint32_t per_chunk = np ? THREADS : THREADS / N;
+    args.n_chunks = (units + per_chunk - 1) / per_chunk;
+    const uint32_t trips = (args.n_chunks + K - 1) / K;
+    args.per_model = trips < 1 ? 1 : trips < blocks ? trips : blocks;   // (an empty range: a block finds nothing)
+    if constexpr (THREADS != kNormThreadsMany)   // (the sizes that the other layout has to itself)
+        if (np) return launch_chained(norm_np_kernel<T, THREADS, K>, args.per_model * N, THREADS, 0, stream, args);
+    if constexpr (THREADS != kAloneThreads)
+        if (!np) return launch_chained(norm_pn_kernel<T, THREADS, K>, args.per_model, THREADS, 0, stream, args);
+    return cudaErrorInvalidValue;
+}
+
+// 64 bytes a thread, or 32 where the grid takes no more than two trips of those.  us with 32 / 64, 1, 3, 10, 30 million values: [P][N] N = 64, 512 threads fp32 6.9 8.3 10.3 25.9 / 6.7
+// 9.3 10.3 24.2, bf16 6.7 9.1 9.8 14.9 / 8.6 9.6 11.7 16.1;  [N][P] N = 2, 40000 and 320000 coordinates bf16 4.1 4.0 / 4.7 4.9.
+template <class T>
+static cudaError_t launch_typed(const NormArgs &args, int sm_count, cudaStream_t stream)
+{
+    constexpr uint32_t kValues = 32 / T::kBytes;   // of a thread in a trip of 32 bytes
+    const uint32_t N = static_cast<uint32_t>(args.pop.N), units = args.unit_hi - args.unit_lo, sm = static_cast<uint32_t>(sm_count);
+    const uint64_t small_trip = static_cast<uint64_t>(kValues) * kNormThreads;
+    if (args.pop.layout == kLayoutNP) {
+        const uint64_t values = 8ull * units;
+        const uint32_t all = norm_blocks_np(T::kCode) * sm, blocks = all < N ? 1u : all / N;
+        if (values <= small_trip) return launch_norm<T, kNormThreads, 32>(args, 1, stream);
+        if (values <= 2 * small_trip) return launch_norm<T, kNormThreads, 64>(args, 1, stream);
+        if (values <= alone_trips(args.pop.N, T::kBytes) * 2ull * kValues * kAloneThreads) return launch_norm<T, kAloneThreads, 64>(args, 1, stream);
+        if (values <= 2 * blocks * small_trip) return launch_norm<T, kNormThreads, 32>(args, blocks, stream);
+        return launch_norm<T, kNormThreads, 64>(args, blocks, stream);
+    }
+    const uint64_t values = 8ull * units * N;
+    if (N > kManyModels) {
+        const uint32_t blocks = 1024 / kNormThreadsMany * sm;
+        if (values <= 2 * blocks * 2 * small_trip) return launch_norm<T, kNormThreadsMany, 32>(args, blocks, stream);
+        return launch_norm<T, kNormThreadsMany, 64>(args, blocks, stream);
+    }
+    const uint32_t blocks = values <= 8 * small_trip ? 1u : 1024 / kNormThreads * sm;
+    if (values <= 2 * blocks * small_trip && blocks > 1) return launch_norm<T, kNormThreads, 32>(args, blocks, stream);
+    return launch_norm<T, kNormThreads, 64>(args, blocks, stream);
+}
 
 cudaError_t launch_grad_norm(NormArgs args, int dtype, int sm_count, cudaStream_t stream)
 {
-    const uint32_t units = args.unit_hi - args.unit_lo, sm = static_cast<uint32_t>(sm_count), N = static_cast<uint32_t>(args.pop.N);
-    const bool np = args.pop.layout == kLayoutNP, f32 = dtype == kDtypeF32;
-    const uint32_t together = f32 ? kTogether<F32> : kTogether<BF16>;
-    const bool alone = np && units > kNormThreadsNP * together && units <= alone_trips_np(args.pop.N) * kAloneThreads * together;
-    const uint32_t per_chunk = np ? (alone ? kAloneThreads : kNormThreadsNP) : kNormThreadsPN / N;
-    args.n_chunks = (units + per_chunk - 1) / per_chunk;
-    const uint32_t trips = (args.n_chunks + together - 1) / together, most = np ? norm_blocks_np(dtype) * sm / N : kNormBlocksPN * sm;
-    args.per_model = trips < most ? trips : most;
-    if (args.per_model < 1 || alone || (!np && trips <= kAloneTripsPN)) args.per_model = 1;   // an empty range: a block finds nothing
-    if (alone) return launch_chained(f32 ? norm_np_kernel<F32, kAloneThreads> : norm_np_kernel<BF16, kAloneThreads>, N, kAloneThreads, 0, stream, args);
-    if (np) return launch_chained(f32 ? norm_np_kernel<F32, kNormThreadsNP> : norm_np_kernel<BF16, kNormThreadsNP>, args.per_model * N, kNormThreadsNP, 0, stream, args);
-    return launch_chained(f32 ? norm_pn_kernel<F32> : norm_pn_kernel<BF16>, args.per_model, kNormThreadsPN, 0, stream, args);
+    return dtype == kDtypeF32 ? launch_typed<F32>(args, sm_count, stream) : launch_typed<BF16>(args, sm_count, stream);
 }
 
 }  // namespace wash

@@ -246,13 +246,13 @@ struct NormArgs {
     double *out;                 // [N]
     uint32_t *status;
 };
-// Blocks of the norm's grid, and the partial sums they leave.
-constexpr int norm_blocks_np(int dtype) { return dtype == kDtypeF32 ? 5 : 4; }   // an SM; five of bf16 have too few registers
-constexpr int kNormBlocksPN = 2;
+// Blocks of the norm's grid on an SM ([N][P]; five of bf16 have too few registers), and the partial sums that a launch leaves at most: [P][N] has blocks of 256
+// threads, four an SM, up to 16 models, and of 512, two, for more.
+constexpr int norm_blocks_np(int dtype) { return dtype == kDtypeF32 ? 5 : 4; }
 inline size_t norm_partials(int layout, int n_models, int sm_count)
 {
     const size_t n = static_cast<size_t>(n_models), sm = static_cast<size_t>(sm_count);
-    return layout == kLayoutNP ? norm_blocks_np(kDtypeF32) * sm + n : kNormBlocksPN * sm * n;
+    return layout == kLayoutNP ? norm_blocks_np(kDtypeF32) * sm + n : 4 * sm * n;
 }
 
 struct ClipArgs {
