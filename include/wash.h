@@ -14,6 +14,9 @@
  *   papa_all                            PAPA-all / DART: every model := the average
  *   wash_consensus_sq                   squared distances to the consensus (Fig. 2)
  *
+ * and, for the training step around them, gradient norms, clipping and the optimizer's step of every
+ * model (wash_grad_norm, wash_clip_grads, wash_sgd_step, wash_adamw_step).
+ *
  * Conventions common to all calls
  *   - Every function returns a wash_status (0 = success, negative = error) and never
  *     throws, aborts or traps.  wash_last_error() gives a message for the last failure

@@ -124,6 +124,15 @@ def _ptr(x) -> Optional[int]:
     raise TypeError("cannot take the address of %r" % type(x))
 
 
+def _norm_ptr(x) -> Optional[int]:
+    """Address of N doubles on the device: a float64 CUDA tensor / int / None."""
+    if x is None or isinstance(x, int):
+        return x
+    if not getattr(x, "is_cuda", False) or x.element_size() != 8 or not x.is_floating_point() or not x.is_contiguous():
+        raise TypeError("norms are contiguous float64 CUDA tensors")
+    return x.data_ptr()
+
+
 _current_raw_stream = None
 
 
@@ -241,11 +250,11 @@ def wash_consensus_sq(ctx, stack: int, tensor_lo: int, tensor_hi: int, dev_sq_ou
 
 def wash_grad_norm(ctx, tensor_lo: int, tensor_hi: int, dev_norm_out, stream=None) -> None:
     """dev_norm_out: [N] doubles on the device, overwritten"""
-    _check(load().wash_grad_norm(ctx, tensor_lo, tensor_hi, _ptr(dev_norm_out), _stream(stream)))
+    _check(load().wash_grad_norm(ctx, tensor_lo, tensor_hi, _norm_ptr(dev_norm_out), _stream(stream)))
 
 
 def wash_clip_grads(ctx, max_norm: float, dev_norm, stream=None) -> None:
-    _check(load().wash_clip_grads(ctx, float(max_norm), _ptr(dev_norm), _stream(stream)))
+    _check(load().wash_clip_grads(ctx, float(max_norm), _norm_ptr(dev_norm), _stream(stream)))
 
 
 def wash_set_decay(ctx, decay_layer=None, stream=None) -> None:
@@ -256,13 +265,13 @@ def wash_set_decay(ctx, decay_layer=None, stream=None) -> None:
 
 def wash_sgd_step(ctx, lr: float, momentum: float = 0.0, weight_decay: float = 0.0, flags: int = 0, max_norm: float = 0.0,
                   dev_norm=None, stream=None) -> None:
-    _check(load().wash_sgd_step(ctx, float(lr), float(momentum), float(weight_decay), flags, float(max_norm), _ptr(dev_norm), _stream(stream)))
+    _check(load().wash_sgd_step(ctx, float(lr), float(momentum), float(weight_decay), flags, float(max_norm), _norm_ptr(dev_norm), _stream(stream)))
 
 
 def wash_adamw_step(ctx, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
                     flags: int = 0, max_norm: float = 0.0, dev_norm=None, stream=None) -> None:
     _check(load().wash_adamw_step(ctx, step, float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), flags, float(max_norm),
-                                  _ptr(dev_norm), _stream(stream)))
+                                  _norm_ptr(dev_norm), _stream(stream)))
 
 
 def wash_step_host(ctx, ops: int, host_params, host_opt, host_avg, step, p, p_layer=None, seed=0, alpha=0.5,

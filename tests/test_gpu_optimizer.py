@@ -436,6 +436,9 @@ def test_refusals():
         refused(B.WASH_ERR_ARG, B.wash_grad_norm, ctx, lo, hi, norm)
     refused(B.WASH_ERR_ARG, B.wash_grad_norm, ctx, 0, 2, None)
     refused(B.WASH_ERR_ARG, B.wash_grad_norm, ctx, 0, 2, norm.data_ptr() + 4)
+    for wrong in (norm.float(), norm.long(), norm.expand(2, 3).t()):
+        with pytest.raises(TypeError):
+            B.wash_grad_norm(ctx, 0, 2, wrong)
     for max_norm in (-1.0, float("nan"), float("inf")):
         refused(B.WASH_ERR_ARG, B.wash_clip_grads, ctx, max_norm, norm)
         refused(B.WASH_ERR_ARG, B.wash_sgd_step, ctx, 0.1, 0.9, 0.0, 0, max_norm, norm)

@@ -38,3 +38,13 @@ def test_adamw_arguments(lib, kw, word):
     with pytest.raises(B.WashError) as e:
         B.wash_adamw_step(None, kw.pop("step", 0), 0.1, stream=0, **kw)
     assert e.value.code == B.WASH_ERR_ARG and word in str(e.value)
+
+
+def test_norms_are_float64_device_tensors(lib):
+    import numpy as np
+    import torch
+    for norm in (torch.zeros(4, dtype=torch.float64), torch.zeros(4), np.zeros(4)):       # host memory would be read by the GPU
+        for call in (lambda: B.wash_grad_norm(None, 0, 1, norm, stream=0), lambda: B.wash_clip_grads(None, 1.0, norm, stream=0),
+                     lambda: B.wash_sgd_step(None, 0.1, max_norm=1.0, dev_norm=norm, stream=0), lambda: B.wash_adamw_step(None, 0, 0.1, max_norm=1.0, dev_norm=norm, stream=0)):
+            with pytest.raises(TypeError):
+                call()
