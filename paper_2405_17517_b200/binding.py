@@ -124,11 +124,18 @@ def _ptr(x) -> Optional[int]:
     raise TypeError("cannot take the address of %r" % type(x))
 
 
+_float64 = None
+
+
 def _norm_ptr(x) -> Optional[int]:
     """Address of N doubles on the device: a float64 CUDA tensor / int / None."""
+    global _float64
     if x is None or isinstance(x, int):
         return x
-    if not getattr(x, "is_cuda", False) or x.element_size() != 8 or not x.is_floating_point() or not x.is_contiguous():
+    if _float64 is None:
+        import torch
+        _float64 = torch.float64
+    if not getattr(x, "is_cuda", False) or x.dtype is not _float64 or not x.is_contiguous():
         raise TypeError("norms are contiguous float64 CUDA tensors")
     return x.data_ptr()
 
