@@ -118,10 +118,9 @@ __device__ __forceinline__ void finish_norms(const NormArgs &a, double *part)
 // values (N apart) fall into one bank (N = 64, 10408 coordinates: 13 us without).
 __device__ __forceinline__ uint32_t spread(uint32_t f) { return (f & ~7u) | ((f ^ (f >> 3) ^ (f >> 6)) & 7u); }
 
-constexpr int kNormThreads = 256;
 // K: octets a thread has in flight
 template <class T, int THREADS, int K>
-__global__ void __launch_bounds__(THREADS, THREADS == kNormThreads ? norm_blocks_np(T::kCode) : 1) norm_np_kernel(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(THREADS, THREADS == kNormThreads ? norm_blocks_np(T::kBytes) : 1) norm_np_kernel(const __grid_constant__ NormArgs a)
 {
     await_previous();
     let_next_start();
@@ -244,60 +243,31 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) norm_pn_kernel(const 
     if (gridDim.x != 1) finish_norms<THREADS>(a, part);
 }
 
-// A small row is not shared out: the blocks' report and the last one's summation take 2 us.  [N][P], us by coordinates, shared / one block of 256 / of 1024 threads:
-// fp32 N = 2 4000 3.8 / 2.2 / 3.0, 10000 3.9 / - / 3.3, 20000 3.9 / - / 4.4;  N = 64 10000 6.5 / - / 3.5, 20000 6.6 / - / 4.4, 40000 7.5 / - / 5.2, 80000 8.6 / - / 6.4 (bf16 9.8 / - / 6.9), 160000
-// 10.5 / - / 9.5;  N = 16 20000 4.2 / - / 4.4, 40000 4.2 / - / 5.2; bf16 N = 2 10000 4.1 / - / 4.5.  [P][N], by values: 8000 4.6 / 3.4, bf16 4.8 / 3.9; 16000 4.5 / 3.8; 20000 bf16 4.7 / 4.6.
-constexpr int kAloneThreads = 1024;
-inline uint32_t alone_trips(int n_models, int bytes) { return n_models >= 48 ? 8u : bytes == 4 ? 1u : 0u; }
-// [P][N]: threads of a block, of which an SM has 1024.  Small blocks start and end sooner, but their partial sums, N a block, take the last one longer.  us with 256 / 512, 1, 3, 10 and 30
-// million values: N = 8 fp32 5.6 7.4 8.9 22.7 / 6.8 7.8 8.6 22.5, bf16 6.1 7.3 9.0 13.6 / 8.9 9.0 10.0 14.5;  N = 16 bf16 6.0 8.0 9.8 14.3 / 8.7 9.2 10.3 14.8;  N = 33 fp32 8.2 9.6 11.7 25.3 / 6.5 8.1 10.0
-// 23.3;  N = 64 fp32 9.8 12.3 13.7 27.2 / 6.7 9.3 10.3 24.2, bf16 7.6 11.9 13.7 18.1 / 8.6 9.6 11.7 16.1.
-constexpr int kManyModels = 16, kNormThreadsMany = 512;
-
 // BYTES of gradients a thread has in flight, THREADS of a block, `blocks` at most for a model ([N][P]) or for all.
 template <class T, int THREADS, int BYTES>
 static cudaError_t launch_norm(NormArgs args, uint32_t blocks, cudaStream_t stream)
 {
     constexpr int K = BYTES / (8 * T::kBytes);
-    const uint32_t N = static_cast<uint32_t>(args.pop.N), units = args.unit_hi - args.unit_lo;
+    const uint32_t N = static_cast<uint32_t>(args.pop.N);
     const bool np = args.pop.layout == kLayoutNP;
-    const uint32_t per_chunk = np ? THREADS : THREADS / N;
-    args.n_chunks = (units + per_chunk - 1) / per_chunk;
-    const uint32_t trips = (args.n_chunks + K - 1) / K;
-    args.per_model = trips < 1 ? 1 : trips < blocks ? trips : blocks;   // (an empty range: a block finds nothing)
+    const NormGrid grid = norm_grid(args.pop.layout, args.pop.N, args.unit_hi - args.unit_lo, THREADS, K, blocks);
+    args.n_chunks = grid.n_chunks;
+    args.per_model = grid.per_model;
     if constexpr (THREADS != kNormThreadsMany)   // (the sizes that the other layout has to itself)
         if (np) return launch_chained(norm_np_kernel<T, THREADS, K>, args.per_model * N, THREADS, 0, stream, args);
-    if constexpr (THREADS != kAloneThreads)
+    if constexpr (THREADS != kNormThreadsAlone)
         if (!np) return launch_chained(norm_pn_kernel<T, THREADS, K>, args.per_model, THREADS, 0, stream, args);
     return cudaErrorInvalidValue;
 }
 
-// 64 bytes a thread, or 32 where the grid takes no more than two trips of those.  us with 32 / 64, 1, 3, 10, 30 million values: [P][N] N = 64, 512 threads fp32 6.9 8.3 10.3 25.9 / 6.7
-// 9.3 10.3 24.2, bf16 6.7 9.1 9.8 14.9 / 8.6 9.6 11.7 16.1;  [N][P] N = 2, 40000 and 320000 coordinates bf16 4.1 4.0 / 4.7 4.9.
 template <class T>
 static cudaError_t launch_typed(const NormArgs &args, int sm_count, cudaStream_t stream)
 {
-    constexpr uint32_t kValues = 32 / T::kBytes;   // of a thread in a trip of 32 bytes
-    const uint32_t N = static_cast<uint32_t>(args.pop.N), units = args.unit_hi - args.unit_lo, sm = static_cast<uint32_t>(sm_count);
-    const uint64_t small_trip = static_cast<uint64_t>(kValues) * kNormThreads;
-    if (args.pop.layout == kLayoutNP) {
-        const uint64_t values = 8ull * units;
-        const uint32_t all = norm_blocks_np(T::kCode) * sm, blocks = all < N ? 1u : all / N;
-        if (values <= small_trip) return launch_norm<T, kNormThreads, 32>(args, 1, stream);
-        if (values <= 2 * small_trip) return launch_norm<T, kNormThreads, 64>(args, 1, stream);
-        if (values <= alone_trips(args.pop.N, T::kBytes) * 2ull * kValues * kAloneThreads) return launch_norm<T, kAloneThreads, 64>(args, 1, stream);
-        if (values <= 2 * blocks * small_trip) return launch_norm<T, kNormThreads, 32>(args, blocks, stream);
-        return launch_norm<T, kNormThreads, 64>(args, blocks, stream);
-    }
-    const uint64_t values = 8ull * units * N;
-    if (N > kManyModels) {
-        const uint32_t blocks = 1024 / kNormThreadsMany * sm;
-        if (values <= 2 * blocks * 2 * small_trip) return launch_norm<T, kNormThreadsMany, 32>(args, blocks, stream);
-        return launch_norm<T, kNormThreadsMany, 64>(args, blocks, stream);
-    }
-    const uint32_t blocks = values <= 8 * small_trip ? 1u : 1024 / kNormThreads * sm;
-    if (values <= 2 * blocks * small_trip && blocks > 1) return launch_norm<T, kNormThreads, 32>(args, blocks, stream);
-    return launch_norm<T, kNormThreads, 64>(args, blocks, stream);
+    const NormPlan plan = norm_plan(args.pop.layout, args.pop.N, args.unit_hi - args.unit_lo, T::kBytes, sm_count);
+    if (plan.threads == kNormThreadsAlone) return launch_norm<T, kNormThreadsAlone, 64>(args, plan.blocks, stream);
+    if (plan.threads == kNormThreadsMany)
+        return plan.bytes == 32 ? launch_norm<T, kNormThreadsMany, 32>(args, plan.blocks, stream) : launch_norm<T, kNormThreadsMany, 64>(args, plan.blocks, stream);
+    return plan.bytes == 32 ? launch_norm<T, kNormThreads, 32>(args, plan.blocks, stream) : launch_norm<T, kNormThreads, 64>(args, plan.blocks, stream);
 }
 
 cudaError_t launch_grad_norm(NormArgs args, int dtype, int sm_count, cudaStream_t stream)

@@ -246,13 +246,61 @@ struct NormArgs {
     double *out;                 // [N]
     uint32_t *status;
 };
-// Blocks of the norm's grid on an SM ([N][P]; five of bf16 have too few registers), and the partial sums that a launch leaves at most: [P][N] has blocks of 256
-// threads, four an SM, up to 16 models, and of 512, two, for more.
-constexpr int norm_blocks_np(int dtype) { return dtype == kDtypeF32 ? 5 : 4; }
+// Threads of a block of the norm's kernels: mostly, of [P][N] with more than kManyModels models, of a block that takes a whole [N][P] row.
+constexpr int kNormThreads = 256, kNormThreadsMany = 512, kNormThreadsAlone = 1024, kManyModels = 16;
+// Blocks of 256 threads on an SM, [N][P]; five of bf16 have too few registers.
+constexpr uint32_t norm_blocks_np(int elem_bytes) { return elem_bytes == 4 ? 5 : 4; }
+
+// How a norm is launched: threads of a block, bytes of gradients a thread has in flight, blocks at most for a model ([N][P]) or for all.
+struct NormPlan {
+    int threads, bytes;
+    uint32_t blocks;
+};
+// A small row is not shared out: the blocks' report and the last one's summation take 2 us.  [N][P], us by coordinates, shared / one block of 256 / of 1024 threads:
+// fp32 N = 2 4000 3.8 / 2.2 / 3.0, 10000 3.9 / - / 3.3, 20000 3.9 / - / 4.4;  N = 64 10000 6.5 / - / 3.5, 20000 6.6 / - / 4.4, 40000 7.5 / - / 5.2, 80000 8.6 / - / 6.4 (bf16 9.8 / - / 6.9), 160000
+// 10.5 / - / 9.5;  N = 16 20000 4.2 / - / 4.4, 40000 4.2 / - / 5.2; bf16 N = 2 10000 4.1 / - / 4.5.  [P][N], by values: 8000 4.6 / 3.4, bf16 4.8 / 3.9; 16000 4.5 / 3.8; 20000 bf16 4.7 / 4.6.
+// [P][N]: threads of a block, of which an SM has 1024.  Small blocks start and end sooner, but their partial sums, N a block, take the last one longer.  us with 256 / 512, 1, 3, 10 and 30
+// million values: N = 8 fp32 5.6 7.4 8.9 22.7 / 6.8 7.8 8.6 22.5, bf16 6.1 7.3 9.0 13.6 / 8.9 9.0 10.0 14.5;  N = 16 bf16 6.0 8.0 9.8 14.3 / 8.7 9.2 10.3 14.8;  N = 33 fp32 8.2 9.6 11.7 25.3 / 6.5 8.1 10.0
+// 23.3;  N = 64 fp32 9.8 12.3 13.7 27.2 / 6.7 9.3 10.3 24.2, bf16 7.6 11.9 13.7 18.1 / 8.6 9.6 11.7 16.1.
+// 64 bytes a thread, or 32 where the grid takes no more than two trips of those.  us with 32 / 64, 1, 3, 10, 30 million values: [P][N] N = 64, 512 threads fp32 6.9 8.3 10.3 25.9 / 6.7
+// 9.3 10.3 24.2, bf16 6.7 9.1 9.8 14.9 / 8.6 9.6 11.7 16.1;  [N][P] N = 2, 40000 and 320000 coordinates bf16 4.1 4.0 / 4.7 4.9.
+inline NormPlan norm_plan(int layout, int n_models, uint32_t units, int elem_bytes, int sm_count)
+{
+    const uint32_t N = static_cast<uint32_t>(n_models), sm = static_cast<uint32_t>(sm_count), thread = 32u / static_cast<uint32_t>(elem_bytes);   // values of a thread in a trip of 32 bytes
+    const uint64_t trip = static_cast<uint64_t>(thread) * kNormThreads;
+    if (layout == kLayoutNP) {
+        const uint64_t values = 8ull * units, alone = n_models >= 48 ? 8 : elem_bytes == 4 ? 1 : 0;   // trips of a block that takes a row
+        const uint32_t all = norm_blocks_np(elem_bytes) * sm, blocks = all < N ? 1u : all / N;
+        if (values <= 2 * trip) return {kNormThreads, values <= trip ? 32 : 64, 1};
+        if (values <= alone * 2 * thread * kNormThreadsAlone) return {kNormThreadsAlone, 64, 1};
+        return {kNormThreads, values <= 2 * blocks * trip ? 32 : 64, blocks};
+    }
+    const uint64_t values = 8ull * units * N;
+    if (n_models > kManyModels) {
+        const uint32_t blocks = 1024 / kNormThreadsMany * sm;
+        return {kNormThreadsMany, values <= 4 * blocks * trip ? 32 : 64, blocks};
+    }
+    const uint32_t blocks = 1024 / kNormThreads * sm;
+    if (values <= 8 * trip) return {kNormThreads, 64, 1};
+    return {kNormThreads, values <= 2 * blocks * trip ? 32 : 64, blocks};
+}
+
+// Chunks of a launch, `together` of which a block takes in a trip, and its blocks (of a model; [P][N]: all).
+struct NormGrid {
+    uint32_t n_chunks, per_model;
+};
+inline NormGrid norm_grid(int layout, int n_models, uint32_t units, int threads, int together, uint32_t blocks)
+{
+    const uint32_t per_chunk = static_cast<uint32_t>(layout == kLayoutNP ? threads : threads / n_models), k = static_cast<uint32_t>(together);
+    const uint32_t chunks = (units + per_chunk - 1) / per_chunk, trips = (chunks + k - 1) / k;
+    return {chunks, trips < 1 ? 1 : trips < blocks ? trips : blocks};   // an empty range: a block finds nothing
+}
+
+// Partial sums that a launch leaves at most, one a block and model.
 inline size_t norm_partials(int layout, int n_models, int sm_count)
 {
     const size_t n = static_cast<size_t>(n_models), sm = static_cast<size_t>(sm_count);
-    return layout == kLayoutNP ? norm_blocks_np(kDtypeF32) * sm + n : 4 * sm * n;
+    return layout == kLayoutNP ? norm_blocks_np(4) * sm + n : 1024 / kNormThreads * sm * n;
 }
 
 struct ClipArgs {

@@ -336,9 +336,11 @@ def test_shards_give_the_whole_populations_step():
     whole.close()
 
 
-def test_a_captured_step_is_replayed():
-    """Norm, step and clipping in one graph on a stream of their own: replays continue from the state they find and read the norms anew."""
-    c = Training(6, [50001, 33], 0, seed=4, decay=[1.0, 0.0])
+@pytest.mark.parametrize("N,layout,wdtype", [(6, 0, "f32"), (6, 1, "f32"), (24, 1, "bf16"), (64, 0, "bf16")])
+def test_a_captured_step_is_replayed(N, layout, wdtype):
+    """Norm, step and clipping in one graph on a stream of their own: replays continue from the state they find and read the norms anew; an
+    eager call of the same context between replays disturbs neither."""
+    c = Training(N, [50001, 33], layout, wdtype, wdtype, seed=4, decay=[1.0, 0.0])
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
     graph = torch.cuda.CUDAGraph()
@@ -358,6 +360,7 @@ def test_a_captured_step_is_replayed():
         oracle.adamw_step(c.ora, 0, c.host["p"], c.host["g"], c.host["m"], c.host["v"], 0.01, weight_decay=0.01, decay=c.decay, max_norm=2.0, norm=norm)
         oracle.clip_grads(c.ora, c.host["g"], 2.0, norm)
         c.assert_equal()
+        assert np.allclose(c.norms(1, 2), oracle.grad_norm(c.ora, c.host["g"], 1, 2), rtol=1e-12, atol=0)
     c.close()
 
 
