@@ -94,7 +94,7 @@ struct wash_ctx {
 
     void *stack_ptr[kStacks] = {};         // by enum wash_stack; entry WASH_STACK_BOTH stays unused
     int stack_dtype[kStacks] = {};
-    double *norm_partial_dev = nullptr;    // wash_grad_norm: the blocks' partial sums; behind them
+    double *norm_partial_dev = nullptr;    // wash_grad_norm: the blocks' partial sums, behind sq_slots_dev in the same allocation; behind them
     uint32_t *norm_ticket_dev = nullptr;   // the number of blocks that have reported, 0 between calls
 
     uint32_t *status_dev = nullptr;
@@ -137,7 +137,6 @@ void release(wash_ctx *ctx)
     if (ctx->status_dev) cudaFree(ctx->status_dev);
     if (ctx->stats_dev) cudaFree(ctx->stats_dev);
     if (ctx->stat_slots_dev) cudaFree(ctx->stat_slots_dev);
-    if (ctx->norm_partial_dev) cudaFree(ctx->norm_partial_dev);
     if (ctx->avg_dev) cudaFree(ctx->avg_dev);
     if (ctx->x_mask) cudaFree(ctx->x_mask);
     if (ctx->x_block_total) cudaFree(ctx->x_block_total);
@@ -569,8 +568,7 @@ int wash_create_segments(wash_ctx **out, int32_t N, int32_t n_segments, const in
         (err = cudaMalloc(&ctx->tile_first_dev, sizeof(uint32_t) * ctx->n_tiles)) != cudaSuccess ||
         (err = cudaMalloc(&ctx->status_dev, sizeof(uint32_t))) != cudaSuccess ||
         (err = cudaMalloc(&ctx->stats_dev, sizeof(wash_stats))) != cudaSuccess ||
-        (err = cudaMalloc(&ctx->stat_slots_dev, slot_bytes)) != cudaSuccess ||
-        (err = cudaMalloc(&ctx->norm_partial_dev, norm_bytes + sizeof(uint32_t))) != cudaSuccess) {
+        (err = cudaMalloc(&ctx->stat_slots_dev, slot_bytes + norm_bytes + sizeof(uint32_t))) != cudaSuccess) {
         release(ctx);
         cudaGetLastError();
         return fail(WASH_ERR_ALLOC, "device allocation failed: %s", cudaGetErrorString(err));
@@ -586,8 +584,7 @@ int wash_create_segments(wash_ctx **out, int32_t N, int32_t n_segments, const in
     if ((err = cudaMemcpy(ctx->tile_first_dev, tile_first.data(), sizeof(uint32_t) * ctx->n_tiles, cudaMemcpyHostToDevice)) != cudaSuccess ||
         (err = cudaMemset(ctx->status_dev, 0, sizeof(uint32_t))) != cudaSuccess ||
         (err = cudaMemset(ctx->stats_dev, 0, sizeof(wash_stats))) != cudaSuccess ||
-        (err = cudaMemset(ctx->stat_slots_dev, 0, slot_bytes)) != cudaSuccess ||
-        (err = cudaMemset(ctx->norm_partial_dev, 0, norm_bytes + sizeof(uint32_t))) != cudaSuccess) {
+        (err = cudaMemset(ctx->stat_slots_dev, 0, slot_bytes + norm_bytes + sizeof(uint32_t))) != cudaSuccess) {
         release(ctx);
         return cuda_fail(err, "table upload");
     }
@@ -598,8 +595,9 @@ int wash_create_segments(wash_ctx **out, int32_t N, int32_t n_segments, const in
         return cuda_fail(err, "table upload");
     }
     ctx->seg_uploaded = true;
-    ctx->norm_ticket_dev = reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(ctx->norm_partial_dev) + norm_bytes);
     ctx->sq_slots_dev = reinterpret_cast<double *>(ctx->stat_slots_dev + wash::kStatSlots + 1);
+    ctx->norm_partial_dev = reinterpret_cast<double *>(reinterpret_cast<char *>(ctx->stat_slots_dev) + slot_bytes);
+    ctx->norm_ticket_dev = reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(ctx->norm_partial_dev) + norm_bytes);
     *out = ctx;
     return WASH_OK;
 }
