@@ -129,15 +129,21 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormThreads ? norm_blocks
     const char *row = static_cast<const char *>(a.grads) + static_cast<size_t>(n) * a.pop.padded_P * T::kBytes;
     double sum[4] = {0.0, 0.0, 0.0, 0.0};
     FullUnits full;
-    const auto load = [&](Octet<T> &g, uint32_t unit) {
-        if (unit < a.unit_hi) g.load(row + static_cast<size_t>(unit) * 8 * T::kBytes);
-        else keep_existing(g, 0u);
-    };
+    constexpr size_t kStride = static_cast<size_t>(THREADS) * 8 * T::kBytes;   // from a thread's octet to its next one
     for (uint32_t c = b * K; c < a.n_chunks; c += a.per_model * K) {
         const uint32_t first = a.unit_lo + c * THREADS, unit = first + threadIdx.x;
+        const char *src = row + static_cast<size_t>(unit) * 8 * T::kBytes;
         Octet<T> g[K];
+        if (first + K * THREADS <= a.unit_hi) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) load(g[k], unit + k * THREADS);
+            for (int k = 0; k < K; ++k) g[k].load(src + k * kStride);
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (unit + k * THREADS < a.unit_hi) g[k].load(src + k * kStride);
+                else keep_existing(g[k], 0u);
+            }
+        }
         if (!one_tensor(a.pop, full, first, K * THREADS, a.status)) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kNormThreads ? norm_blocks
                 const uint32_t unit = a.unit_lo + (c + k) * THREADS + threadIdx.x;
                 if (unit >= a.unit_hi) continue;
                 Octet<T> g;
-                load(g, unit);
+                g.load(row + static_cast<size_t>(unit) * 8 * T::kBytes);
                 keep_existing(g, existing(find_place(a.pop, unit, a.status), unit));
                 found |= specials(g);
             }
@@ -186,22 +192,30 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) norm_pn_kernel(const 
     let_next_start();
     __shared__ double part[8 * THREADS];
     const uint32_t N = static_cast<uint32_t>(a.pop.N), units = THREADS / N, octets = units * N;
-    const uint32_t e0 = 8u * threadIdx.x / N, n0 = 8u * threadIdx.x - e0 * N;
+    const uint32_t octet = min(threadIdx.x, octets - 1u);   // the last threads repeat the chunk's last octet; nobody reads their sums
+    const uint32_t e0 = 8u * octet / N, n0 = 8u * octet - e0 * N;
     double sum[8];   // of model (n0 + q) mod N
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum[q] = 0.0;
     FullUnits full;
     // of the chunk whose first unit is `first`
-    const auto there = [&](uint32_t first) { return threadIdx.x < octets && first < a.unit_hi && (units <= a.unit_hi - first || threadIdx.x < (a.unit_hi - first) * N); };
-    const auto load = [&](Octet<T> &g, uint32_t first) {
-        if (there(first)) g.load(static_cast<const char *>(a.grads) + (static_cast<size_t>(first) * N + threadIdx.x) * 8 * T::kBytes);
-        else keep_existing(g, 0u);
-    };
+    const auto there = [&](uint32_t first) { return first < a.unit_hi && (units <= a.unit_hi - first || octet < (a.unit_hi - first) * N); };
+    const size_t stride = static_cast<size_t>(octets) * 8 * T::kBytes;   // from a thread's octet to its next one
+    const auto at = [&](uint32_t first) { return static_cast<const char *>(a.grads) + (static_cast<size_t>(first) * N + octet) * 8 * T::kBytes; };
     for (uint32_t c = blockIdx.x * K; c < a.n_chunks; c += gridDim.x * K) {
         const uint32_t first = a.unit_lo + c * units;
+        const char *src = at(first);
         Octet<T> g[K];
+        if (first + K * units <= a.unit_hi) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) load(g[k], first + k * units);
+            for (int k = 0; k < K; ++k) g[k].load(src + k * stride);
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (there(first + k * units)) g[k].load(src + k * stride);
+                else keep_existing(g[k], 0u);
+            }
+        }
         if (!one_tensor(a.pop, full, first, K * units, a.status)) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -225,7 +239,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) norm_pn_kernel(const 
                 if (!there(first)) continue;
                 Octet<T> g;
                 float decay[8];
-                load(g, first);
+                g.load(at(first));
                 keep_existing(g, existing_pn<false>(a.pop, first, e0, n0, a.unit_hi, a.status, decay));
                 found |= specials(g);
             }
