@@ -4,7 +4,7 @@
 //
 // The number of blocks: a resident grid (one wave) reads and writes in step and loses a quarter of the bandwidth (fp32 [N][P], ResNet-50 N = 10: 1 wave 425 us, 4 365, 8 337,
 // 16 326, a trip a block 311 = 6.58 TB/s), but blocks that find nothing to clip cost, too (1 wave 3.5 us, 16 9.4, a trip a block 46).  [P][N], whose threads look up eight factors
-// first: fp32 N = 8 8 waves 250 us, 16 245, a trip a block 253; bf16 134, 133, 179.
+// first: fp32 N = 8 8 waves 250 us, 16 245, a trip a block 253; bf16 134 and 133.
 #include "wash_octet.cuh"
 
 namespace wash {

@@ -115,7 +115,7 @@ __device__ __forceinline__ void finish_norms(const NormArgs &a, double *part)
 }
 
 // Where a block's value f lies in shared memory: eight neighbours trade places, so that neither the threads' writes (8 values apart) nor the reads of a model's
-// values (N apart) fall into one bank (N = 64, 10408 coordinates: 13 us without).
+// values (N apart) fall into one bank (N = 64, 10408 coordinates: 12 -> 9.4 us).
 __device__ __forceinline__ uint32_t spread(uint32_t f) { return (f & ~7u) | ((f ^ (f >> 3) ^ (f >> 6)) & 7u); }
 
 // K: octets a thread has in flight

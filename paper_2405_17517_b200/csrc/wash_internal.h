@@ -257,8 +257,8 @@ struct NormPlan {
     uint32_t blocks;
 };
 // A small row is not shared out: the blocks' report and the last one's summation take 2 us.  [N][P], us by coordinates, shared / one block of 256 / of 1024 threads:
-// fp32 N = 2 4000 3.8 / 2.2 / 3.0, 10000 3.9 / - / 3.3, 20000 3.9 / - / 4.4;  N = 64 10000 6.5 / - / 3.5, 20000 6.6 / - / 4.4, 40000 7.5 / - / 5.2, 80000 8.6 / - / 6.4 (bf16 9.8 / - / 6.9), 160000
-// 10.5 / - / 9.5;  N = 16 20000 4.2 / - / 4.4, 40000 4.2 / - / 5.2; bf16 N = 2 10000 4.1 / - / 4.5.  [P][N], by values: 8000 4.6 / 3.4, bf16 4.8 / 3.9; 16000 4.5 / 3.8; 20000 bf16 4.7 / 4.6.
+// fp32 N = 2 4000 3.8 / 2.2 / 3.0, 10000 4.2 / - / 3.3, 20000 3.9 / - / 4.4;  N = 64 10000 6.5 / - / 3.5, 20000 6.6 / - / 4.4, 40000 7.5 / - / 5.2, 80000 8.6 / - / 6.4 (bf16 9.8 / - / 6.9), 160000
+// 10.5 / - / 9.5;  N = 16 40000 4.2 / - / 5.2; bf16 N = 2 10000 4.1 / - / 4.5.  [P][N], by values: 8000 4.6 / 3.4, bf16 4.8 / 3.9; 16000 4.5 / 3.8; 20000 bf16 4.7 / 4.6.
 // [P][N]: threads of a block, of which an SM has 1024.  Small blocks start and end sooner, but their partial sums, N a block, take the last one longer.  us with 256 / 512, 1, 3, 10 and 30
 // million values: N = 8 fp32 5.6 7.4 8.9 22.7 / 6.8 7.8 8.6 22.5, bf16 6.1 7.3 9.0 13.6 / 8.9 9.0 10.0 14.5;  N = 16 bf16 6.0 8.0 9.8 14.3 / 8.7 9.2 10.3 14.8;  N = 33 fp32 8.2 9.6 11.7 25.3 / 6.5 8.1 10.0
 // 23.3;  N = 64 fp32 9.8 12.3 13.7 27.2 / 6.7 9.3 10.3 24.2, bf16 7.6 11.9 13.7 18.1 / 8.6 9.6 11.7 16.1.

@@ -129,7 +129,7 @@ __device__ __forceinline__ Place find_place(const PopView &pop, uint32_t unit, u
     return at;
 }
 // The same for every lane of a warp, all lanes calling, their units ascending: the lanes fetch the entries of 32 tensors at once, from the first lane's tile on, and
-// pick theirs by shuffles -- two trips to the L2 instead of one a tensor (norms of five models with 12 small tensors 6.0 -> 4.9 us).
+// pick theirs by shuffles -- two trips to the L2 instead of one a tensor (the SGD step of five models with 12 small tensors 3.3 -> 2.3 us in a graph).
 __device__ __forceinline__ Place warp_place(const PopView &pop, uint32_t unit, uint32_t *status)
 {
     constexpr uint32_t kAll = 0xFFFFFFFFu;
