@@ -596,3 +596,33 @@ def test_norms_of_extreme_values_in_long_rows(P, dtype, layout):
     assert torch.allclose(out[[0, 1, 4]], want[[0, 1, 4]], rtol=2 * P * 2.0 ** -53, atol=0)
     assert out[2] == float("inf") and out[3].isnan() and out[5].isnan()
     pop.close()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("wdtype,gdtype", [("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("N", [2, 3, 8, 19, 64])
+def test_padding_is_neither_read_nor_written(N, wdtype, gdtype, layout):
+    """Padding of finite numbers, which a result would take up and a store would change: every bit of it stays, in every stack."""
+    for numel in (RAGGED, ODD, [1], [4093, 2]):
+        c = Training(N, numel, layout, wdtype, gdtype, seed=N, decay=_decay(len(numel)))
+        real = np.zeros(c.P, bool)
+        for d, o in zip(c.numel, c.off):
+            real[o:o + d] = True
+        pad = torch.from_numpy(np.flatnonzero(~real)).cuda()
+        rows = {r: (t.view(N, c.P) if layout == 0 else t.view(c.P, N).t()) for r, t in c.dev.items()}
+        for k, r in enumerate("pgmv"):
+            rows[r][:, pad] = 77.0 + k
+        norm = c.norms().copy()
+        assert np.allclose(norm, oracle.grad_norm(c.ora, c.host["g"]), rtol=1e-12, atol=0)
+        bound = 0.5 * float(norm.min())
+        _step(c, "sgd", 0.9, True, 0, bound, norm)
+        _step(c, "adamw", 0.9, False, 1, bound, norm)
+        _step(c, "sgd", 0.0, False, 0, bound, norm)
+        B.wash_clip_grads(c.gpu.ctx, bound, c.norm)
+        oracle.clip_grads(c.ora, c.host["g"], bound, norm)
+        for k, r in enumerate("pgmv"):
+            assert (rows[r][:, pad] == 77.0 + k).all(), r
+            want = W.from_stack(c.host[r], N, c.numel, c.off, c.P, layout)
+            want = W.bf16_bits_to_f32(want) if want.dtype == np.uint16 else want
+            assert (c.dense_of(r).view(np.uint32) == want.view(np.uint32)).all(), r
+        c.close()
