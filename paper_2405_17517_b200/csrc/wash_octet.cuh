@@ -17,17 +17,6 @@ struct Octet {
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) v[i] = F32::load_group(p + 16 * i);
     }
-    // the same for what is not used again soon: it leaves the caches first
-    __device__ __forceinline__ void load_once(const char *p)
-    {
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) v[i] = __ldcs(reinterpret_cast<const uint4 *>(p + 16 * i));
-    }
-    __device__ __forceinline__ void store_once(char *p) const
-    {
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) __stcs(reinterpret_cast<uint4 *>(p + 16 * i), v[i]);
-    }
     __device__ __forceinline__ void store(char *p) const
     {
 #pragma unroll
