@@ -33,6 +33,10 @@
  *     Launches of the ordinary kind and copies need nothing.
  *     Calls on one context must be issued on one stream at a time (the context's
  *     tables are rewritten in stream order when the probabilities change).
+ *   - Shuffles and wash_exchange_plan captured into a graph keep their probabilities, whatever eager
+ *     calls and other graphs of the context use before or between replays: the first capture of a set
+ *     of probabilities allocates a table for it (32 bytes a tensor), which lives until wash_destroy.
+ *     A graph must not be replayed after that, nor beside another call of its context.
  *   - Randomness is a pure function of (seed, step, tensor index, coordinate index)
  *     through Philox4x32-10, so a result does not depend on layout, dtype, grid size,
  *     kernel variant, or on which of the shuffle entry points produced it.

@@ -6,6 +6,7 @@
 #include <cstring>
 #include <new>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include <cuda.h>
@@ -74,6 +75,18 @@ struct DeviceGuard {
     }
 };
 
+// A segment table with the thresholds of a call, and the coordinates that they select in expectation.
+struct CallTable {
+    const SegEntry *dev = nullptr;
+    double expected = 0.0;
+};
+// The table of calls that were captured into graphs.
+struct CapturedTable {
+    std::vector<uint64_t> thr;
+    SegEntry *dev = nullptr;
+    double expected = 0.0;
+};
+
 }  // namespace
 
 struct wash_ctx {
@@ -91,6 +104,7 @@ struct wash_ctx {
     cudaEvent_t slot_event[kSlots] = {nullptr, nullptr, nullptr, nullptr};
     bool slot_used[kSlots] = {false, false, false, false};
     int next_slot = 0;
+    std::vector<CapturedTable> captured;   // one per set of thresholds, never changed; graphs hold their addresses
 
     void *stack_ptr[kStacks] = {};         // by enum wash_stack; entry WASH_STACK_BOTH stays unused
     int stack_dtype[kStacks] = {};
@@ -133,6 +147,7 @@ void release(wash_ctx *ctx)
     if (!ctx) return;
     DeviceGuard guard(ctx->device);
     if (ctx->seg_dev) cudaFree(ctx->seg_dev);
+    for (const CapturedTable &t : ctx->captured) cudaFree(t.dev);
     if (ctx->tile_first_dev) cudaFree(ctx->tile_first_dev);
     if (ctx->status_dev) cudaFree(ctx->status_dev);
     if (ctx->stats_dev) cudaFree(ctx->stats_dev);
@@ -254,9 +269,55 @@ int upload_table(wash_ctx *ctx, cudaStream_t stream)
     return WASH_OK;
 }
 
-// Brings the device copy of the segment table up to date with the call's
-// probabilities (uploaded, in stream order, only when they changed).
-int sync_table(wash_ctx *ctx, double p, const double *p_layer, cudaStream_t stream)
+// The table of a call that is being captured: one of its own for every set of thresholds, uploaded now and kept until wash_destroy.  A copy recorded into the
+// graph would put this call's thresholds, and the decay multipliers of now, over those of later calls at every replay; without one, a replay
+// would run with the thresholds of the eager call before it.
+int captured_table(wash_ctx *ctx, double p, const double *p_layer, CallTable *out)
+try {
+    std::vector<uint64_t> thr(static_cast<size_t>(ctx->n_seg));
+    for (int s = 0; s < ctx->n_seg; ++s) thr[static_cast<size_t>(s)] = threshold_of(p_layer ? p_layer[s] : p);
+    for (const CapturedTable &t : ctx->captured)
+        if (t.thr == thr) {
+            out->dev = t.dev;
+            out->expected = t.expected;
+            return WASH_OK;
+        }
+    CapturedTable t;
+    std::vector<SegEntry> entries = ctx->seg_host;
+    for (size_t s = 0; s < entries.size(); ++s) {
+        entries[s].thr = thr[s];
+        t.expected += static_cast<double>(entries[s].numel) * static_cast<double>(thr[s]) / 4294967296.0;
+    }
+    t.thr = std::move(thr);
+    ctx->captured.reserve(ctx->captured.size() + 1);   // nothing throws once the table exists
+    // Allocations and work on other streams are open to a capturing thread in the relaxed mode; neither becomes part of the graph.
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaError_t err = cudaThreadExchangeStreamCaptureMode(&mode);
+    if (err != cudaSuccess) return cuda_fail(err, "cudaThreadExchangeStreamCaptureMode");
+    const size_t bytes = sizeof(SegEntry) * entries.size();
+    cudaStream_t side = nullptr;
+    if ((err = cudaMalloc(&t.dev, bytes)) == cudaSuccess && (err = cudaStreamCreateWithFlags(&side, cudaStreamNonBlocking)) == cudaSuccess &&
+        (err = cudaMemcpyAsync(t.dev, entries.data(), bytes, cudaMemcpyHostToDevice, side)) == cudaSuccess)
+        err = cudaStreamSynchronize(side);
+    if (side) cudaStreamDestroy(side);
+    if (err != cudaSuccess && t.dev) cudaFree(t.dev);
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (err != cudaSuccess) {
+        cudaGetLastError();
+        return err == cudaErrorMemoryAllocation ? fail(WASH_ERR_ALLOC, "device allocation of a captured call's table failed: %s", cudaGetErrorString(err))
+                                                : cuda_fail(err, "upload of a captured call's table");
+    }
+    out->dev = t.dev;
+    out->expected = t.expected;
+    ctx->captured.push_back(std::move(t));
+    return WASH_OK;
+} catch (const std::bad_alloc &) {
+    return fail(WASH_ERR_ALLOC, "out of host memory");
+}
+
+// The segment table with the call's probabilities: the context's own, uploaded in stream order when they
+// changed, or, while the stream is being captured, one that stays.
+int table_of(wash_ctx *ctx, double p, const double *p_layer, cudaStream_t stream, CallTable *out)
 {
     // every probability is checked before the first threshold of the host mirror changes: a
     // rejected call must leave the mirror equal to the device table
@@ -264,6 +325,13 @@ int sync_table(wash_ctx *ctx, double p, const double *p_layer, cudaStream_t stre
         const double ps = p_layer ? p_layer[s] : p;
         if (!(ps >= 0.0 && ps <= 1.0)) return fail(WASH_ERR_ARG, "probability of tensor %d is %g, not in [0,1]", s, ps);
     }
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    const cudaError_t err = cudaStreamIsCapturing(stream, &status);
+    if (err != cudaSuccess) {
+        cudaGetLastError();
+        return cuda_fail(err, "cudaStreamIsCapturing");
+    }
+    if (status != cudaStreamCaptureStatusNone) return captured_table(ctx, p, p_layer, out);
     bool changed = !ctx->seg_uploaded;
     for (int s = 0; s < ctx->n_seg; ++s) {
         const uint64_t thr = threshold_of(p_layer ? p_layer[s] : p);
@@ -272,12 +340,17 @@ int sync_table(wash_ctx *ctx, double p, const double *p_layer, cudaStream_t stre
             changed = true;
         }
     }
-    if (!changed) return WASH_OK;
-    ctx->seg_uploaded = false;   // until the copy below is queued, the mirror is ahead of the device table
-    ctx->expected_selected = 0.0;
-    for (int s = 0; s < ctx->n_seg; ++s)
-        ctx->expected_selected += static_cast<double>(ctx->seg_host[s].numel) * static_cast<double>(ctx->seg_host[s].thr) / 4294967296.0;
-    return upload_table(ctx, stream);
+    if (changed) {
+        ctx->seg_uploaded = false;   // until the copy below is queued, the mirror is ahead of the device table
+        ctx->expected_selected = 0.0;
+        for (int s = 0; s < ctx->n_seg; ++s)
+            ctx->expected_selected += static_cast<double>(ctx->seg_host[s].numel) * static_cast<double>(ctx->seg_host[s].thr) / 4294967296.0;
+        const int rc = upload_table(ctx, stream);
+        if (rc != WASH_OK) return rc;
+    }
+    out->dev = ctx->seg_dev;
+    out->expected = ctx->expected_selected;
+    return WASH_OK;
 }
 
 // [P][N]: a vector of padding after a group of the streaming kernels' shared-memory image, against bank conflicts.  It
@@ -301,13 +374,6 @@ uint32_t pn_pad(const wash_ctx *ctx, bool bf16, bool two_stacks, float share)
 uint32_t sq_pad(const wash_ctx *ctx)
 {
     return ctx->layout == WASH_LAYOUT_PN && ctx->N > 2 && !(ctx->N & 1) ? 4u : 0u;
-}
-
-int ensure_table(wash_ctx *ctx, cudaStream_t stream)
-{
-    if (ctx->seg_uploaded) return WASH_OK;
-    std::vector<double> zeros(static_cast<size_t>(ctx->n_seg), 0.0);
-    return sync_table(ctx, 0.0, zeros.data(), stream);
 }
 
 // which: 0 = parameters, 1 = optimizer state, 2 = both
@@ -334,11 +400,13 @@ int shuffle_impl(wash_ctx *ctx, int which, uint64_t step, double p, const double
     DeviceGuard guard(ctx->device);
     if (guard.err != cudaSuccess) return cuda_fail(guard.err, "cudaSetDevice");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    int rc = sync_table(ctx, p, p_layer, stream);
+    CallTable table;
+    int rc = table_of(ctx, p, p_layer, stream, &table);
     if (rc != WASH_OK) return rc;
 
     wash::ShuffleArgs args;
     args.pop = view_of(ctx);
+    args.pop.seg = table.dev;
     args.a = a;
     args.b = b;
     args.group_lo = group_lo;
@@ -355,7 +423,7 @@ int shuffle_impl(wash_ctx *ctx, int which, uint64_t step, double p, const double
         const double bytes = static_cast<double>(ctx->N) * static_cast<double>(ctx->padded_P) *
                              (elem_bytes(a_dtype) + (b ? elem_bytes(b_dtype) : 0));
         const double kernel_ns = bytes / 6000.0 + 2000.0;
-        const double reporting_blocks = std::fmin(ctx->expected_selected, static_cast<double>(ctx->n_groups) / 64.0);
+        const double reporting_blocks = std::fmin(table.expected, static_cast<double>(ctx->n_groups) / 64.0);
         args.stat_slots = ctx->stat_slots_dev;
         args.stats_direct = 2.0 * reporting_blocks / kernel_ns <= 0.35;
         // WASH_MODE_AUTO: the expected share of selected coordinates decides
@@ -363,17 +431,17 @@ int shuffle_impl(wash_ctx *ctx, int which, uint64_t step, double p, const double
             double coordinates = 0.0;
             for (int s = 0; s < ctx->n_seg; ++s) coordinates += static_cast<double>(ctx->seg_host[s].numel);
             const double share = sparse_share(ctx->layout, ctx->N, b != nullptr, a_dtype == wash::kDtypeBF16);
-            mode = ctx->expected_selected < share * coordinates ? WASH_MODE_SPARSE : WASH_MODE_STREAM;
+            mode = table.expected < share * coordinates ? WASH_MODE_SPARSE : WASH_MODE_STREAM;
         }
         double coordinates = 0.0;
         for (int s = 0; s < ctx->n_seg; ++s) coordinates += static_cast<double>(ctx->seg_host[s].numel);
-        args.expected_share = coordinates > 0.0 ? static_cast<float>(ctx->expected_selected / coordinates) : 0.f;
+        args.expected_share = coordinates > 0.0 ? static_cast<float>(table.expected / coordinates) : 0.f;
         args.pn_pad = pn_pad(ctx, a_dtype == wash::kDtypeBF16, b != nullptr, args.expected_share);
         // The streaming kernel's early flavour (permutations drawn while the copies are in flight, dense
         // serving for N > 16) costs registers and, for N > 16, three more permutation columns of shared
         // memory per thread: measured, it pays only for large populations of which most coordinates are
         // served (kEarlyShare).
-        args.early = ctx->N > 16 && ctx->expected_selected >= kEarlyShare * coordinates && wash::stored_together(ctx->layout, ctx->N) == 1;
+        args.early = ctx->N > 16 && table.expected >= kEarlyShare * coordinates && wash::stored_together(ctx->layout, ctx->N) == 1;
         if (ctx->shape.blocks_per_sm == -2) args.early = false;   // tuning override (wash_set_launch)
         if (ctx->shape.blocks_per_sm == -3) args.early = true;
         if (sq) {   // the statistic is gathered by the streaming kernel only
@@ -407,8 +475,6 @@ int reduce_impl(wash_ctx *ctx, int op, int stack, void *out, int out_dtype, floa
     DeviceGuard guard(ctx->device);
     if (guard.err != cudaSuccess) return cuda_fail(guard.err, "cudaSetDevice");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    int rc = ensure_table(ctx, stream);
-    if (rc != WASH_OK) return rc;
     wash::ReduceArgs args;
     args.pop = view_of(ctx);
     args.stack = ctx->stack_ptr[stack];
@@ -736,8 +802,6 @@ int wash_consensus_sq(wash_ctx *ctx, int32_t stack, int32_t tensor_lo, int32_t t
     DeviceGuard guard(ctx->device);
     if (guard.err != cudaSuccess) return cuda_fail(guard.err, "cudaSetDevice");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    int rc = ensure_table(ctx, stream);
-    if (rc != WASH_OK) return rc;
     // the streaming shuffle's statistic with nothing selected
     wash::ShuffleArgs args = {};
     args.pop = view_of(ctx);
@@ -1225,12 +1289,14 @@ int wash_exchange_plan(wash_ctx *ctx, uint64_t step, double p, const double *p_l
     DeviceGuard guard(ctx->device);
     if (guard.err != cudaSuccess) return cuda_fail(guard.err, "cudaSetDevice");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    int rc = sync_table(ctx, p, p_layer, stream);
+    CallTable table;
+    int rc = table_of(ctx, p, p_layer, stream, &table);
     if (rc != WASH_OK) return rc;
     ctx->x_step = step;
     ctx->x_seed = seed;
     wash::ExchangeArgs args;
     if ((rc = exchange_args(ctx, &args)) != WASH_OK) return rc;
+    args.pop.seg = table.dev;   // (the plan is all that reads thresholds)
     cudaError_t err = wash::launch_exchange_plan(args, stream);
     if (err != cudaSuccess) return cuda_fail(err, "exchange plan launch");
     ctx->x_planned = true;
