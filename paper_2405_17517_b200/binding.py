@@ -104,10 +104,23 @@ def _i64(a):
     return arr, arr.ctypes.data_as(ctypes.POINTER(ctypes.c_int64))
 
 
-def _dbl_or_null(a):
+# What the library reads and writes by a context's sizes is measured against them here: handle -> (models, tensors, device).
+_contexts: dict = {}
+
+
+def _known(ctx: int, N: int, n_tensors: int, device: int) -> int:
+    _contexts[ctx] = (int(N), n_tensors, int(device))
+    return ctx
+
+
+def _per_tensor(a, ctx):
+    """An array of one double per tensor of the context (or None) and its address"""
     if a is None:
         return None, None
     arr = np.ascontiguousarray(a, dtype=np.float64)
+    sizes = _contexts.get(ctx)
+    if sizes is not None and arr.size < sizes[1]:
+        raise ValueError("%d values given, the context has %d tensors" % (arr.size, sizes[1]))
     return arr, arr.__array_interface__["data"][0]
 
 
@@ -127,16 +140,23 @@ def _ptr(x) -> Optional[int]:
 _float64 = None
 
 
-def _norm_ptr(x) -> Optional[int]:
-    """Address of N doubles on the device: a float64 CUDA tensor / int / None."""
+def _norm_ptr(x, ctx) -> Optional[int]:
+    """Address of N doubles on the context's device: a float64 CUDA tensor / int / None."""
     global _float64
     if x is None or isinstance(x, int):
         return x
     if _float64 is None:
         import torch
         _float64 = torch.float64
-    if not getattr(x, "is_cuda", False) or x.dtype is not _float64 or not x.is_contiguous():
+    try:
+        fits, device = x.dtype is _float64 and x.is_contiguous(), x.get_device()
+    except AttributeError:
+        fits, device = False, -1
+    if not fits or device < 0:
         raise TypeError("norms are contiguous float64 CUDA tensors")
+    N, _, home = _contexts.get(ctx) or (0, 0, device)
+    if x.numel() < N or device != home:
+        raise ValueError("%d norms on device %d given, the context has %d models on device %d" % (x.numel(), device, N, home))
     return x.data_ptr()
 
 
@@ -168,7 +188,7 @@ def wash_create(N: int, numel: Sequence[int], layout: int = WASH_LAYOUT_NP, devi
     arr, p = _i64(numel)
     ctx = ctypes.c_void_p()
     _check(load().wash_create(ctypes.byref(ctx), N, arr.size, p, layout, device))
-    return ctx.value
+    return _known(ctx.value, N, arr.size, device)
 
 
 def wash_create_segments(N: int, numel, tensor_id=None, coord_begin=None, layout: int = WASH_LAYOUT_NP, device: int = 0) -> int:
@@ -180,10 +200,11 @@ def wash_create_segments(N: int, numel, tensor_id=None, coord_begin=None, layout
         ctypes.byref(ctx), N, arr.size, p,
         None if tid is None else tid.ctypes.data_as(ctypes.POINTER(ctypes.c_uint32)),
         None if cb is None else cb.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)), layout, device))
-    return ctx.value
+    return _known(ctx.value, N, arr.size, device)
 
 
 def wash_destroy(ctx: int) -> None:
+    _contexts.pop(ctx, None)
     _check(load().wash_destroy(ctx))
 
 
@@ -214,7 +235,7 @@ def wash_layer_probs(L: int, p: float, schedule: int = WASH_SCHEDULE_DECREASING)
 
 
 def _shuffle(fn, ctx, step, p, p_layer, seed, stream, stats):
-    keep, pl = _dbl_or_null(p_layer)
+    keep, pl = _per_tensor(p_layer, ctx)
     _check(fn(ctx, step, float(p), pl, seed, _stream(stream), _ptr(stats)))
 
 
@@ -233,7 +254,7 @@ def wash_shuffle_both(ctx, step, p, p_layer=None, seed=0, stream=None, stats=Non
 def wash_shuffle_consensus(ctx, stacks: int, step, p, p_layer=None, seed=0, stream=None, stats=None,
                            tensor_bounds=(0, 0), dev_sq_out=None) -> None:
     """tensor_bounds: n_ranges + 1 ascending tensor indices; dev_sq_out: [n_ranges][N] doubles on the device"""
-    keep, pl = _dbl_or_null(p_layer)
+    keep, pl = _per_tensor(p_layer, ctx)
     tb = np.ascontiguousarray(tensor_bounds, dtype=np.int32)
     _check(load().wash_shuffle_consensus(ctx, stacks, step, float(p), pl, seed, _stream(stream), _ptr(stats), tb.size - 1,
                                          tb.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), _ptr(dev_sq_out)))
@@ -257,34 +278,34 @@ def wash_consensus_sq(ctx, stack: int, tensor_lo: int, tensor_hi: int, dev_sq_ou
 
 def wash_grad_norm(ctx, tensor_lo: int, tensor_hi: int, dev_norm_out, stream=None) -> None:
     """dev_norm_out: [N] doubles on the device, overwritten"""
-    _check(load().wash_grad_norm(ctx, tensor_lo, tensor_hi, _norm_ptr(dev_norm_out), _stream(stream)))
+    _check(load().wash_grad_norm(ctx, tensor_lo, tensor_hi, _norm_ptr(dev_norm_out, ctx), _stream(stream)))
 
 
 def wash_clip_grads(ctx, max_norm: float, dev_norm, stream=None) -> None:
-    _check(load().wash_clip_grads(ctx, float(max_norm), _norm_ptr(dev_norm), _stream(stream)))
+    _check(load().wash_clip_grads(ctx, float(max_norm), _norm_ptr(dev_norm, ctx), _stream(stream)))
 
 
 def wash_set_decay(ctx, decay_layer=None, stream=None) -> None:
     """decay_layer: a multiplier of the steps' weight decay per tensor; None: 1 for all"""
-    keep, dl = _dbl_or_null(decay_layer)
+    keep, dl = _per_tensor(decay_layer, ctx)
     _check(load().wash_set_decay(ctx, dl, _stream(stream)))
 
 
 def wash_sgd_step(ctx, lr: float, momentum: float = 0.0, weight_decay: float = 0.0, flags: int = 0, max_norm: float = 0.0,
                   dev_norm=None, stream=None) -> None:
-    _check(load().wash_sgd_step(ctx, float(lr), float(momentum), float(weight_decay), flags, float(max_norm), _norm_ptr(dev_norm), _stream(stream)))
+    _check(load().wash_sgd_step(ctx, float(lr), float(momentum), float(weight_decay), flags, float(max_norm), _norm_ptr(dev_norm, ctx), _stream(stream)))
 
 
 def wash_adamw_step(ctx, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
                     flags: int = 0, max_norm: float = 0.0, dev_norm=None, stream=None) -> None:
     _check(load().wash_adamw_step(ctx, step, float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), flags, float(max_norm),
-                                  _norm_ptr(dev_norm), _stream(stream)))
+                                  _norm_ptr(dev_norm, ctx), _stream(stream)))
 
 
 def wash_step_host(ctx, ops: int, host_params, host_opt, host_avg, step, p, p_layer=None, seed=0, alpha=0.5,
                    stream=None):
     """-> (selected_coords, moved_values) of this call"""
-    keep, pl = _dbl_or_null(p_layer)
+    keep, pl = _per_tensor(p_layer, ctx)
     st = wash_stats(0, 0)
     _check(load().wash_step_host(ctx, ops, _ptr(host_params), _ptr(host_opt), _ptr(host_avg), step, float(p), pl,
                                  seed, ctypes.c_float(alpha), _stream(stream), ctypes.byref(st)))
@@ -295,7 +316,9 @@ def wash_shuffle_noalloc(N: int, numel, layout: int, dtype: int, dev_stack, n_el
                          p_layer=None, seed: int = 0, device: int = 0, stream=None, stats=None) -> None:
     """The streaming shuffle without a context and without any allocation (see wash.h)."""
     arr, np_ = _i64(numel)
-    keep, pl = _dbl_or_null(p_layer)
+    keep, pl = _per_tensor(p_layer, None)
+    if keep is not None and keep.size < arr.size:
+        raise ValueError("%d probabilities given for %d tensors" % (keep.size, arr.size))
     rc = load().wash_shuffle_noalloc(N, arr.size, np_, layout, dtype, _ptr(dev_stack), n_elems, step, float(p), pl,
                                      seed, device, _stream(stream), _ptr(stats))
     if rc != WASH_OK:
@@ -333,7 +356,7 @@ def wash_exchange_staging_open(ctx, stack: int, parity: int, handles) -> None:
 
 
 def wash_exchange_plan(ctx, step: int, p: float, p_layer=None, seed: int = 0, stream=None) -> None:
-    keep, pl = _dbl_or_null(p_layer)
+    keep, pl = _per_tensor(p_layer, ctx)
     _check(load().wash_exchange_plan(ctx, step, float(p), pl, seed, _stream(stream)))
 
 
