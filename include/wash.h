@@ -288,7 +288,7 @@ enum wash_step_flags {
  *     d = (weight_decay * decay_t) p + c_n g;   m <- momentum m + d;   p <- p - lr u
  * with u = m, with WASH_STEP_NESTEROV u = d + momentum m, and with momentum = 0 u = d (the optimizer-state stack is then
  * neither needed nor touched).  Zeros are the state before the first step.
- *   lr, weight_decay   not negative; momentum in [0,1)
+ *   lr, weight_decay   not negative; momentum in [0,1), also once rounded to binary32 (below 1 - 2^-25)
  *   dev_norm           DEVICE array of N doubles: c_n as in wash_clip_grads, with the gradients themselves left as they are;
  *                      NULL: c_n = 1 and max_norm is ignored
  * Evaluated in binary32: products that are added to something are fused with the addition (one rounding), every other operation is rounded
@@ -302,7 +302,7 @@ int wash_sgd_step(wash_ctx *ctx, double lr, double momentum, double weight_decay
  * WASH_STACK_OPT2.  step counts from 0, as in wash_shuffle; t = step + 1:
  *     g' = c_n g;   m <- beta1 m + (1 - beta1) g';   v <- beta2 v + ((1 - beta2) g') g'
  *     p <- p - lr ( (m / (1 - beta1^t)) / (sqrt(v) / sqrt(1 - beta2^t) + eps) + (weight_decay * decay_t) p )
- * beta1, beta2 in [0,1), eps positive; the factors of the bias correction are computed in binary64 and multiplied in binary32.  Otherwise as wash_sgd_step.
+ * beta1, beta2 in [0,1) as momentum is, eps positive; the factors of the bias correction are computed in binary64 and multiplied in binary32.  Otherwise as wash_sgd_step.
  * A shuffle exchanges the stacks that it is given: for WASH+Opt with Adam shuffle both moments (the second one through a context of its own
  * that has it bound as a stack; equal seed, step and probabilities give it the same permutations). */
 int wash_adamw_step(wash_ctx *ctx, uint64_t step, double lr, double beta1, double beta2, double eps, double weight_decay,

@@ -494,6 +494,8 @@ int reduce_impl(wash_ctx *ctx, int op, int stack, void *out, int out_dtype, floa
 
 // a non-negative number that binary32 holds (rounded)
 bool fits_f32(double x) { return x >= 0.0 && x <= 3.4028234663852886e38; }
+// a moving average's weight: in [0,1) as the kernels hold it, too (1 would never forget, while new terms are still added)
+bool is_average_weight(double x) { return x >= 0.0 && static_cast<float>(x) < 1.f; }
 
 bool capturing(cudaStream_t stream)
 {
@@ -896,7 +898,7 @@ int wash_set_decay(wash_ctx *ctx, const double *decay_layer, void *stream_v)
 
 int wash_sgd_step(wash_ctx *ctx, double lr, double momentum, double weight_decay, int32_t flags, double max_norm, const double *dev_norm, void *stream)
 {
-    if (!(momentum >= 0.0 && momentum < 1.0)) return fail(WASH_ERR_ARG, "momentum is %g, not in [0,1)", momentum);
+    if (!is_average_weight(momentum)) return fail(WASH_ERR_ARG, "momentum is %.9g, not in [0,1) in binary32", momentum);
     if (flags & ~(WASH_STEP_NESTEROV | WASH_STEP_SKIP_NONFINITE)) return fail(WASH_ERR_ARG, "unknown bits in flags");
     if ((flags & WASH_STEP_NESTEROV) && momentum == 0.0) return fail(WASH_ERR_ARG, "Nesterov's form needs a momentum above 0");
     wash::StepArgs args = {};
@@ -909,8 +911,8 @@ int wash_adamw_step(wash_ctx *ctx, uint64_t step, double lr, double beta1, doubl
                     const double *dev_norm, void *stream)
 {
     if (step >> 56) return fail(WASH_ERR_ARG, "step must be below 2^56");
-    if (!(beta1 >= 0.0 && beta1 < 1.0)) return fail(WASH_ERR_ARG, "beta1 is %g, not in [0,1)", beta1);
-    if (!(beta2 >= 0.0 && beta2 < 1.0)) return fail(WASH_ERR_ARG, "beta2 is %g, not in [0,1)", beta2);
+    if (!is_average_weight(beta1)) return fail(WASH_ERR_ARG, "beta1 is %.9g, not in [0,1) in binary32", beta1);
+    if (!is_average_weight(beta2)) return fail(WASH_ERR_ARG, "beta2 is %.9g, not in [0,1) in binary32", beta2);
     if (!(fits_f32(eps) && static_cast<float>(eps) > 0.f)) return fail(WASH_ERR_ARG, "eps is %g, not a positive binary32 number", eps);
     if (flags & ~WASH_STEP_SKIP_NONFINITE) return fail(WASH_ERR_ARG, "unknown bits in flags");
     wash::StepArgs args = {};
