@@ -288,7 +288,8 @@ enum wash_step_flags {
  *     d = (weight_decay * decay_t) p + c_n g;   m <- momentum m + d;   p <- p - lr u
  * with u = m, with WASH_STEP_NESTEROV u = d + momentum m, and with momentum = 0 u = d (the optimizer-state stack is then
  * neither needed nor touched).  Zeros are the state before the first step.
- *   lr, weight_decay   not negative; momentum in [0,1), also once rounded to binary32 (below 1 - 2^-25)
+ *   lr, weight_decay   not negative, binary32 numbers, weight_decay also times the largest multiplier of wash_set_decay (a graph's
+ *                      replays are not checked against multipliers set later); momentum in [0,1), also once rounded to binary32 (below 1 - 2^-25)
  *   dev_norm           DEVICE array of N doubles: c_n as in wash_clip_grads, with the gradients themselves left as they are;
  *                      NULL: c_n = 1 and max_norm is ignored
  * Evaluated in binary32: products that are added to something are fused with the addition (one rounding), every other operation is rounded

@@ -98,6 +98,7 @@ struct wash_ctx {
 
     std::vector<SegEntry> seg_host;        // thresholds as last uploaded
     bool seg_uploaded = false;
+    float largest_decay = 1.f;             // of the table's multipliers
     SegEntry *seg_dev = nullptr;
     uint32_t *tile_first_dev = nullptr;
     SegEntry *seg_pinned[kSlots] = {nullptr, nullptr, nullptr, nullptr};
@@ -526,6 +527,8 @@ int step_impl(wash_ctx *ctx, wash::StepArgs &args, int rule, double lr, double w
     if (!ctx) return fail(WASH_ERR_ARG, "ctx is NULL");
     if (!fits_f32(lr)) return fail(WASH_ERR_ARG, "lr is %g, not a non-negative binary32 number", lr);
     if (!fits_f32(weight_decay)) return fail(WASH_ERR_ARG, "weight_decay is %g, not a non-negative binary32 number", weight_decay);
+    if (!std::isfinite(static_cast<float>(weight_decay) * ctx->largest_decay))   // times a weight of 0 it would be NaN
+        return fail(WASH_ERR_ARG, "weight_decay %g times the largest multiplier %g is not a binary32 number", weight_decay, static_cast<double>(ctx->largest_decay));
     int rc;
     if (dev_norm && (rc = check_clipping(max_norm, dev_norm)) != WASH_OK) return rc;
     if (!dev_norm && (flags & WASH_STEP_SKIP_NONFINITE)) return fail(WASH_ERR_ARG, "WASH_STEP_SKIP_NONFINITE needs dev_norm");
@@ -886,8 +889,10 @@ int wash_set_decay(wash_ctx *ctx, const double *decay_layer, void *stream_v)
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     if (capturing(stream)) return fail(WASH_ERR_STATE, "the decay multipliers cannot be set while the stream is being captured");
     bool changed = !ctx->seg_uploaded;
+    ctx->largest_decay = 0.f;
     for (int s = 0; s < ctx->n_seg; ++s) {
         const float decay = decay_layer ? static_cast<float>(decay_layer[s]) : 1.f;
+        ctx->largest_decay = std::fmax(ctx->largest_decay, decay);
         changed = changed || decay != ctx->seg_host[s].decay;
         ctx->seg_host[s].decay = decay;
     }
