@@ -291,13 +291,26 @@ def wash_set_decay(ctx, decay_layer=None, stream=None) -> None:
     _check(load().wash_set_decay(ctx, dl, _stream(stream)))
 
 
-def wash_sgd_step(ctx, lr: float, momentum: float = 0.0, weight_decay: float = 0.0, flags: int = 0, max_norm: float = 0.0,
+def _no_bound(dev_norm) -> float:
+    """A step without a bound on the norms: there is none to go with norms, since 0 would take all gradients away."""
+    if dev_norm is not None:
+        raise ValueError("dev_norm needs a max_norm")
+    return 0.0
+
+
+def wash_sgd_step(ctx, lr: float, momentum: float = 0.0, weight_decay: float = 0.0, flags: int = 0, max_norm: Optional[float] = None,
                   dev_norm=None, stream=None) -> None:
+    """max_norm: needed with dev_norm, ignored without it"""
+    if max_norm is None:
+        max_norm = _no_bound(dev_norm)
     _check(load().wash_sgd_step(ctx, float(lr), float(momentum), float(weight_decay), flags, float(max_norm), _norm_ptr(dev_norm, ctx), _stream(stream)))
 
 
 def wash_adamw_step(ctx, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
-                    flags: int = 0, max_norm: float = 0.0, dev_norm=None, stream=None) -> None:
+                    flags: int = 0, max_norm: Optional[float] = None, dev_norm=None, stream=None) -> None:
+    """max_norm: needed with dev_norm, ignored without it"""
+    if max_norm is None:
+        max_norm = _no_bound(dev_norm)
     _check(load().wash_adamw_step(ctx, step, float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), flags, float(max_norm),
                                   _norm_ptr(dev_norm, ctx), _stream(stream)))
 

@@ -10,14 +10,15 @@ from paper_2405_17517_b200 import binding as B
 
 
 class Library:
-    """Takes every call and keeps the names; contexts are numbered from 4096."""
+    """Takes every call and keeps the names and the last arguments; contexts are numbered from 4096."""
 
     def __init__(self):
-        self.calls, self.made = [], 0
+        self.calls, self.made, self.last = [], 0, ()
 
     def __getattr__(self, name):
         def call(*args):
             self.calls.append(name)
+            self.last = args
             if name in ("wash_create", "wash_create_segments"):
                 self.made += 1
                 args[0]._obj.value = 4096 * self.made
@@ -107,3 +108,25 @@ def test_a_destroyed_contexts_sizes_are_forgotten(library):
     other = B.wash_create(2, [5])
     B.wash_set_decay(other, [1.0], stream=0)
     B.wash_grad_norm(other, 0, 1, Norms(2, 0), stream=0)
+
+
+def test_norms_come_with_a_bound(library):
+    """A step that is given norms and no bound would run with the bound 0, which takes all gradients away."""
+    ctx = B.wash_create(4, [5, 6, 7])
+    before = list(library.calls)
+    for norm in (Norms(4, 0), 1 << 20):
+        for call in (lambda: B.wash_sgd_step(ctx, 0.1, 0.9, dev_norm=norm, stream=0), lambda: B.wash_adamw_step(ctx, 0, 0.1, dev_norm=norm, stream=0),
+                     lambda: B.wash_sgd_step(ctx, 0.1, flags=B.WASH_STEP_SKIP_NONFINITE, dev_norm=norm, stream=0)):
+            with pytest.raises(ValueError):
+                call()
+    assert library.calls == before
+    for bound in (0.0, 0, 2.5):                                          # 0 is what it says when it is asked for
+        B.wash_sgd_step(ctx, 0.1, 0.9, 0.0, 0, bound, Norms(4, 0), stream=0)
+        assert library.last[5] == bound and library.last[6] == 1 << 20
+        B.wash_adamw_step(ctx, 0, 0.1, max_norm=bound, dev_norm=Norms(4, 0), stream=0)
+        assert library.last[8] == bound and library.last[9] == 1 << 20
+    for bound in (None, 0.0, 2.5):                                       # ignored without norms
+        B.wash_sgd_step(ctx, 0.1, 0.9, max_norm=bound, stream=0)
+        assert library.last[6] is None
+        B.wash_adamw_step(ctx, 0, 0.1, max_norm=bound, stream=0)
+        assert library.last[9] is None
