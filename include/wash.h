@@ -258,7 +258,8 @@ int wash_consensus_sq(wash_ctx *ctx, int32_t stack, int32_t tensor_lo, int32_t t
  * Every model has its own gradient norm and its own clipping factor.  All calls are kernel launches on `stream` and can be captured into a
  * graph; a graph holds the arguments of its calls (learning rate, step), but reads dev_norm, the stacks and the table of wash_set_decay as they
  * are when it is replayed.  wash_grad_norm uses a workspace of the context: calls of one context, replayed graphs that hold them among those, must
- * not overlap on the GPU.  wash_set_mode and wash_set_launch do not apply. */
+ * not overlap on the GPU.  wash_set_mode and wash_set_launch do not apply.  The calls need whole stacks (wash_bind): a context of the one-model-per-device
+ * form, whose worker has one row (wash_exchange_bind), cannot make them. */
 
 /* The gradient norm of every model over tensors [tensor_lo, tensor_hi):
  *     dev_norm_out[n] = sqrt( sum_i g_n,i^2 )
@@ -269,7 +270,8 @@ int wash_grad_norm(wash_ctx *ctx, int32_t tensor_lo, int32_t tensor_hi, double *
 
 /* Clips the gradients in place, each model by its own norm:
  *     c_n = min(1, max_norm / (dev_norm[n] + 1e-6)), rounded to binary32;   g_n <- c_n g_n
- * dev_norm: DEVICE array of N doubles (from wash_grad_norm); max_norm: finite, not negative.  Models with c_n = 1 are not touched.  A
+ * dev_norm: DEVICE array of N doubles, none negative (from wash_grad_norm); max_norm: finite, not negative.  Models with c_n = 1 keep
+ * every bit; in WASH_LAYOUT_PN their values beside a clipped model's are read and written back, so nothing else may write them meanwhile.  A
  * norm that is NaN makes its model's gradients NaN, an infinite one makes them 0 (NaN where they are infinite).  bf16 gradients are
  * widened, multiplied and rounded to nearest even.  A step below takes the factor itself; this call is for other consumers of the gradients. */
 int wash_clip_grads(wash_ctx *ctx, double max_norm, const double *dev_norm, void *stream);
@@ -281,7 +283,8 @@ int wash_set_decay(wash_ctx *ctx, const double *decay_layer, void *stream);
 
 enum wash_step_flags {
     WASH_STEP_NESTEROV = 1,      /* wash_sgd_step only                                               */
-    WASH_STEP_SKIP_NONFINITE = 2 /* a model whose dev_norm is infinite or NaN keeps weights and state */
+    WASH_STEP_SKIP_NONFINITE = 2 /* a model whose dev_norm is infinite or NaN keeps weights and state
+                                    bit by bit (WASH_LAYOUT_PN: read and written back)             */
 };
 
 /* One step of SGD on every model, in place on the parameter stack and, with momentum, the optimizer-state stack:

@@ -1,10 +1,11 @@
-// Clipping: the gradients of the models whose factor is below 1 are multiplied by it, in place; the other models' bits stay as they are.
+// Clipping: the gradients of the models whose factor is below 1 are multiplied by it, in place; the other models' bits stay as they are (in [P][N] those that share an octet
+// with a clipped model's are written back as they were read: an octet's store is one or two 16-byte pieces).
 // Bound by HBM: the clipped models' gradients are read and written once.  The grid walks the chunks from the last to the first: wash_grad_norm, which ran
 // before, went from the first to the last and left the last in the L2.
 //
 // The number of blocks: a resident grid (one wave) reads and writes in step and loses a quarter of the bandwidth (fp32 [N][P], ResNet-50 N = 10: 1 wave 425 us, 4 365, 8 337,
 // 16 326, a trip a block 311 = 6.58 TB/s), but blocks that find nothing to clip cost, too (1 wave 3.5 us, 16 9.4, a trip a block 46).  [P][N], whose threads look up eight factors
-// first: fp32 N = 8 8 waves 250 us, 16 245, a trip a block 253; bf16 134 and 133.
+// first: fp32 N = 8 8 waves 250 us, 16 245, a trip a block 253; bf16 134 and 133.  bf16 [N][P] N = 8 129 us (6.35 TB/s), half of the models 65, none 10.
 #include "wash_octet.cuh"
 
 namespace wash {

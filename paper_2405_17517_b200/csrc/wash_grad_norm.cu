@@ -4,8 +4,8 @@
 // One pass: a resident grid walks the chunks, a thread adds up its octets' squares, a block leaves one partial sum a model, and the block that reports last
 // adds the blocks' partials and takes the root.  [N][P]: a block has one model, five of 256 threads an SM (four for bf16).  [P][N]: a block has them all; there are 1024 threads an SM, in
 // four blocks or two.
-// Bound by HBM in fp32 (ResNet-50 N = 10 147 us = 6.95 TB/s, [P][N] N = 8 120 us = 6.8), nearly so in bf16, whose bytes hold twice the
-// values and keep two issue slots in three busy (N = 8 67 us = 6.1 TB/s, [P][N] 67 to 68).
+// Bound by HBM in fp32 (ResNet-50 N = 10, norm behind norm, 147 us = 6.97 TB/s, [P][N] N = 8 120 us = 6.8), nearly so in bf16: a trip of as many bytes
+// holds twice the values and keeps half of the issue slots busy, during which its warp has no loads in flight (N = 8 67 us = 6.1 TB/s, [P][N] 67).
 #include "wash_octet.cuh"
 
 namespace wash {

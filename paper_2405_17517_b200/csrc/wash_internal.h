@@ -256,14 +256,51 @@ struct NormPlan {
     int threads, bytes;
     uint32_t blocks;
 };
-// A small row is not shared out: the blocks' report and the last one's summation take 2 us.  [N][P], us by coordinates, shared / one block of 256 / of 1024 threads:
-// fp32 N = 2 4000 3.8 / 2.2 / 3.0, 10000 4.2 / - / 3.3, 20000 3.9 / - / 4.4;  N = 64 10000 6.5 / - / 3.5, 20000 6.6 / - / 4.4, 40000 7.5 / - / 5.2, 80000 8.6 / - / 6.4 (bf16 9.8 / - / 6.9), 160000
-// 10.5 / - / 9.5;  N = 16 40000 4.2 / - / 5.2; bf16 N = 2 10000 4.1 / - / 4.5.  [P][N], by values: 8000 4.6 / 3.4, bf16 4.8 / 3.9; 16000 4.5 / 3.8; 20000 bf16 4.7 / 4.6.
-// [P][N]: threads of a block, of which an SM has 1024.  Small blocks start and end sooner, but their partial sums, N a block, take the last one longer.  us with 256 / 512, 1, 3, 10 and 30
-// million values: N = 8 fp32 5.6 7.4 8.9 22.7 / 6.8 7.8 8.6 22.5, bf16 6.1 7.3 9.0 13.6 / 8.9 9.0 10.0 14.5;  N = 16 bf16 6.0 8.0 9.8 14.3 / 8.7 9.2 10.3 14.8;  N = 33 fp32 8.2 9.6 11.7 25.3 / 6.5 8.1 10.0
-// 23.3;  N = 64 fp32 9.8 12.3 13.7 27.2 / 6.7 9.3 10.3 24.2, bf16 7.6 11.9 13.7 18.1 / 8.6 9.6 11.7 16.1.
-// 64 bytes a thread, or 32 where the grid takes no more than two trips of those.  us with 32 / 64, 1, 3, 10, 30 million values: [P][N] N = 64, 512 threads fp32 6.9 8.3 10.3 25.9 / 6.7
-// 9.3 10.3 24.2, bf16 6.7 9.1 9.8 14.9 / 8.6 9.6 11.7 16.1;  [N][P] N = 2, 40000 and 320000 coordinates bf16 4.1 4.0 / 4.7 4.9.
+// Times below: one B200, us a call, call after call (one block to a row: N = 16, 32, 47 and 64 from a graph of calls).
+//
+// One block to a row ([N][P]), against blocks that share it and report (the report and the last block's summation take 2 us).  By population and coordinates:
+//                          shared   one block of 256   one of 1024 threads
+//   fp32 N =  2    4000      3.8          2.2                3.0
+//                 10000      4.2           -                 3.3
+//                 20000      3.9           -                 4.4
+//   fp32 N = 16   10000      4.2           -                 3.4
+//                 40000      4.4           -                 4.9
+//   fp32 N = 32   40000      4.6           -                 4.9
+//                 80000      5.1           -                 6.1
+//   fp32 N = 47   40000      4.9           -                 4.9
+//                 80000      6.2           -                 6.1
+//                131072      6.2           -                 6.8
+//   fp32 N = 64   40000      5.2           -                 4.9
+//                 80000      6.5           -                 6.1
+//                131072      6.5           -                 6.8
+//                160000      8.0           -                 8.7
+//   bf16 N =  2   10000      4.1           -                 4.5
+//   bf16 N = 16   32768      3.6           -                 3.0
+//                 40000      4.2           -                 5.6
+//   bf16 N = 47   80000      5.4           -                 6.5
+//                131072      5.7           -                 5.6
+//   bf16 N = 64   80000      7.5           -                 6.5
+//                131072      6.0           -                 5.7
+//                160000      8.4           -                 8.2
+//                262144      8.0           -                 9.1
+// A row's time in one block does not depend on N, shared it grows with the partial sums: fp32 meets at N = 40 to 48 from 40000 to 80000 coordinates; beyond that, and in bf16 between N = 48 and 64
+// off the multiples of 8192 coordinates, the rule loses up to a microsecond either way.
+//
+// One block to all ([P][N], up to 16 models), by values: shared / one block   8000 4.6 / 3.4, bf16 4.8 / 3.9;  16000 4.5 / 3.8;  bf16 20000 4.7 / 4.6.
+//
+// Threads of a block, [P][N], of which an SM has 1024.  Small blocks start and end sooner, but their partial sums, N a block, take the last one longer.  256 / 512 threads:
+//   values          1e6         3e6         1e7         3e7
+//   fp32 N =  8   5.6 / 6.8   7.4 / 7.8   8.9 / 8.6  22.7 / 22.5
+//   bf16 N =  8   6.1 / 8.9   7.3 / 9.0   9.0 / 10.0 13.6 / 14.5
+//   bf16 N = 16   6.0 / 8.7   8.0 / 9.2   9.8 / 10.3 14.3 / 14.8
+//   fp32 N = 33   8.2 / 6.5   9.6 / 8.1  11.7 / 10.0 25.3 / 23.3
+//   fp32 N = 64   9.8 / 6.7  12.3 / 9.3  13.7 / 10.3 27.2 / 24.2
+//   bf16 N = 64   7.6 / 8.6  11.9 / 9.6  13.7 / 11.7 18.1 / 16.1
+//
+// Bytes a thread has in flight: 64, or 32 where the grid takes no more than two trips of those.  32 / 64 bytes:
+//   [P][N] N = 64, 512 threads   fp32 6.9 / 6.7   8.3 / 9.3  10.3 / 10.3  25.9 / 24.2   (1e6, 3e6, 1e7, 3e7 values)
+//                                bf16 6.7 / 8.6   9.1 / 9.6   9.8 / 11.7  14.9 / 16.1
+//   [N][P] N = 2                 bf16 4.1 / 4.7   4.0 / 4.9                             (40000, 320000 coordinates)
 inline NormPlan norm_plan(int layout, int n_models, uint32_t units, int elem_bytes, int sm_count)
 {
     const uint32_t N = static_cast<uint32_t>(n_models), sm = static_cast<uint32_t>(sm_count), thread = 32u / static_cast<uint32_t>(elem_bytes);   // values of a thread in a trip of 32 bytes

@@ -2,14 +2,14 @@
 //   SGD    d = c g + wd_t p;  m <- mu m + d;  p <- p - lr u,  u = m, with Nesterov d + mu m, without momentum d
 //   AdamW  g' = c g;  m <- b1 m + (1 - b1) g';  v <- b2 v + (1 - b2) g'^2;
 //          p <- p - lr (s1 m / (s2 sqrt(v) + eps) + wd_t p),  s1 = 1 / (1 - b1^t), s2 = 1 / sqrt(1 - b2^t)
-// in binary32, products fused with the additions behind them (explicit _rn intrinsics), bf16 weights rounded to nearest even at the store: the step costs nothing more than the
-// bytes it moves, so nothing is approximated (quotient and root as the hardware's approximations: AdamW of bf16 weights 716 -> 686 us, fp32 the same).
+// in binary32, products fused with the additions behind them (explicit _rn intrinsics), bf16 weights rounded to nearest even at the store: large steps cost the bytes they
+// move, so nothing is approximated (quotient and root as the hardware's approximations: AdamW of ResNet-50 N = 8 bf16 [P][N] 664 -> 649 us, [N][P] and fp32 the same).
 //
 // Bound by HBM: one trip a thread, an octet of every stack, all loads in flight before anything else (a lookup of the tensor in front of the barrier costs a
 // tenth).  Blocks of 256 threads go from the last chunk to the first, as wash_clip.cu has it; the norm's pass leaves little in the L2 that lasts until the step
 // has come to it (ResNet-18 N = 5 norm and step: 214 us in the norm's order, 210 in this; loads and stores marked as used once, or with an evict-first policy: the same or slower).
-// ResNet-50, us and share of the measured copy rate: SGD with momentum N = 10 fp32 753 (104 %), N = 8 bf16 428 (102 %), [P][N] N = 8 582 (107 %) and 410 (107 %);
-// AdamW N = 10 fp32 1084 (101 %), N = 8 bf16 682 (101 %), [P][N] N = 8 849 (103 %) and 689 (100 %).
+// ResNet-50, us and share of the measured copy rate: SGD with momentum N = 10 fp32 755 (103 %), N = 8 bf16 434 (101 %), [P][N] N = 8 583 (107 %) and 416 (105 %);
+// AdamW N = 10 fp32 1086 (101 %), N = 8 bf16 678 (101 %), [P][N] N = 8 831 (105 %) and 666 (103 %).
 #include "wash_octet.cuh"
 
 namespace wash {
@@ -84,7 +84,7 @@ struct StepOctet {
     }
 };
 
-// Blocks an SM holds at least, by the registers that are left to a thread then.  us with 1 / 4 / 5 / 6:
+// Blocks an SM holds at least, by the registers that are left to a thread then ([P][N] AdamW fp32: 4 spill 48 bytes a thread, and are faster for it).  us with 1 / 4 / 5 / 6:
 //   [N][P], 1 / 5 / 6 / 7  ResNet-50 N = 10 fp32 without momentum 467 / 463 / 464 / 446, with 760 / 757 / 767 / 938, AdamW 1082 / 1087 / 1186 / 1618;
 //           N = 8 bf16 243 / 243 / 255 / 220, 438 / 461 / 437 / 439 (fp32 gradients 522 / 494 / 479 / 538), 699 / 678 / 710 / 852
 //   [P][N]  ResNet-50 N = 8  momentum fp32 582 / 583 / 591 / 661, bf16 439 / 443 / 410 / 415, bf16 and fp32 474 / 470 / 466 / 525;  without fp32 370 / 371 / 348 / 349, bf16
