@@ -434,6 +434,8 @@ class Population:
     def bind(self, stack: int, tensor) -> None:
         if not tensor.is_cuda or not tensor.is_contiguous():
             raise ValueError("a stack must be a contiguous CUDA tensor")
+        if tensor.get_device() != self.device:
+            raise ValueError("the stack is on device %d, the population on device %d" % (tensor.get_device(), self.device))
         wash_bind(self.ctx, stack, _torch_dtype_code(tensor), tensor, tensor.numel())
         self._stacks[stack] = tensor   # keep it alive while bound
 

@@ -48,9 +48,17 @@ class Norms:
 
 @pytest.fixture
 def library(monkeypatch):
-    lib = Library()
+    lib, populations, start = Library(), [], B.Population.__init__
+
+    def kept(self, *args, **kw):
+        populations.append(self)
+        start(self, *args, **kw)
+
     monkeypatch.setattr(B, "load", lambda: lib)
-    return lib
+    monkeypatch.setattr(B.Population, "__init__", kept)
+    yield lib
+    for population in populations:      # a made-up handle must not reach the library itself
+        population.close()
 
 
 def _norm_calls(ctx, norm):
@@ -130,3 +138,17 @@ def test_norms_come_with_a_bound(library):
         assert library.last[6] is None
         B.wash_adamw_step(ctx, 0, 0.1, max_norm=bound, stream=0)
         assert library.last[9] is None
+
+
+def test_stacks_lie_on_the_populations_device(library):
+    """The kernels run on the context's device; a stack of another one is memory that they may not reach."""
+    pop = B.Population(4, [5, 6, 7], 0, 1)
+    before = list(library.calls)
+    for role in (B.WASH_STACK_PARAMS, B.WASH_STACK_OPT, B.WASH_STACK_GRADS, B.WASH_STACK_OPT2):
+        for device in (0, 2):
+            with pytest.raises(ValueError):
+                pop.bind(role, Norms(96, device, torch.float32))
+    assert library.calls == before
+    for role in (B.WASH_STACK_PARAMS, B.WASH_STACK_OPT, B.WASH_STACK_GRADS, B.WASH_STACK_OPT2):
+        pop.bind(role, Norms(96, 1, torch.float32))
+    assert library.calls == before + ["wash_bind"] * 4
